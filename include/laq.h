@@ -454,6 +454,108 @@ laq_status laq_embed(const void *E, const int32_t *tokens, int64_t M, int64_t V,
 laq_status laq_argmax(const void *logits, int64_t M, int64_t V, int32_t *out, void *stream);
 
 /* ======================================================================================
+ * A serving step over a paged cache: the operations a decoder needs between its projections when
+ * many requests, each with any number of new tokens (a prompt, a chunk of one, a draft, one token),
+ * run in one batch, and the sampled choice of the next token.  The paper defines none of them; each
+ * follows the definition stated below.  Sums, softmax statistics and norms are kept in fp32 or in
+ * whole numbers; a stored value is rounded once.  The conventions are those of the decoder
+ * operations above: device memory of the caller, host checks first, device values clamped.
+ * ====================================================================================== */
+
+/* Types of the tensors that these calls read and write. */
+#define LAQ_F16 0
+#define LAQ_BF16 1
+#define LAQ_F32 2 /* laq_sample's logits only */
+
+/*
+ * The paged cache and the batch that works on it.  Keys and values live in pages of page_size
+ * tokens (a power of two, 8 .. 1024), Hkv heads and D = 128 elements a token: element d of slot s of
+ * page p and head g is at p * page_stride + g * head_stride + s * token_stride + d, for k and for v
+ * (strides in elements, multiples of 8, token_stride and head_stride at least D, each stride below
+ * 2^38: [pages][Hkv][page_size][D] and [pages][page_size][Hkv][D], or the halves of one buffer of
+ * both, are given by their strides).  Both bases 16-byte aligned.
+ *   Request b of `batch` holds kv_len[b] tokens, its new ones last; token t is in slot
+ * t % page_size of page block_table[b * table_stride + t / page_size].  The new tokens of request
+ * b are rows q_start[b] .. q_start[b + 1] - 1 of the batch's rows (q_start[0] = 0, nondecreasing,
+ * batch + 1 entries); n such rows are at positions kv_len[b] - n .. kv_len[b] - 1.
+ *   Device values are clamped: kv_len to [0, max_pages * page_size]; rows outside the batch's and
+ * table entries that no token needs are not touched; a needed page outside [0, pages) is not
+ * written and reads as zeros.  The tables are 4-byte aligned; max_pages * page_size < 2^31.
+ */
+typedef struct laq_paged_kv {
+    void *k, *v;
+    const int32_t *block_table; /* [batch][table_stride], max_pages entries of a row in use */
+    const int32_t *q_start;     /* [batch + 1] */
+    const int32_t *kv_len;      /* [batch] */
+    int64_t pages, page_stride, head_stride, token_stride;
+    int64_t batch, table_stride, max_pages;
+    int32_t page_size, Hkv, D, dtype; /* LAQ_F16 or LAQ_BF16: k, v and the rows */
+} laq_paged_kv;
+
+/*
+ * laq_paged_append -- per-head RMSNorm of q and k, rotary embedding, and the append of k and v to the
+ * pages, for the T rows of the batch.  Row r of qkv holds (Hq + 2 Hkv) heads of D elements (q, k, v)
+ * at r * qkv_stride (elements, a multiple of 4, at least (Hq + 2 Hkv) * D; 8-byte aligned base).
+ *   q_h = rope(norm(q_h, q_norm_w), p) -> q_out [T][Hq][D];  k_g = rope(norm(k_g, k_norm_w), p) and
+ *   v_g -> the slot of position p;  norm(x, w) = x / sqrt(mean(x^2) + eps) * w (w: [D], 8-byte
+ *   aligned, of the rows' type), x itself where w is NULL.
+ * rope turns the pairs (i, i + D/2) by p * theta^(-2i/D), as laq_qk_norm_rope; the angle is reduced
+ * in 64-bit whole turns first, so that a position of any size costs no precision.  A row whose
+ * position is negative (more new tokens than kv_len) writes q_out and nothing else, a row of no
+ * request nothing.  T in 0..2^24, Hq a multiple of Hkv, theta > 1, eps >= 0.
+ */
+laq_status laq_paged_append(const laq_paged_kv *kv, const void *qkv, int64_t qkv_stride, int64_t T,
+                            int32_t Hq, const void *q_norm_w, const void *k_norm_w, float theta,
+                            float eps, void *q_out, void *stream);
+
+/* Bytes of workspace laq_paged_attention needs; 0 for invalid sizes. */
+size_t laq_paged_attention_workspace_bytes(int64_t T, int64_t batch, int64_t max_q, int32_t Hq,
+                                           int32_t Hkv);
+
+/*
+ * laq_paged_attention -- grouped-query attention of the batch's new tokens over the paged cache,
+ * causal within each request: for the row at position p of request b and q head h,
+ *   out[row][h] = sum_{t <= p} softmax_t(scale * q[row][h] . k[t][g]) v[t][g],  g = h / (Hq / Hkv),
+ * over the request's cached tokens (the new ones are read from the cache too: append them first).
+ * A row that sees no token (p < 0) gets zeros; a row of no request is not written.
+ *   q    [T][Hq][D] at row stride q_stride (elements, a multiple of 8, at least Hq * D), 16-byte
+ *        aligned, of the cache's type.  out [T][Hq][D], dense, 16-byte aligned.
+ *   max_q  at least the most new tokens of any request (rows past it in a request are not written).
+ *   Hq / Hkv <= 64, scale > 0 and finite, T and batch up to 2^24.
+ * Values of tokens at positions that a row does not see must be finite where they belong to the
+ * request (t < kv_len[b]); what lies in its pages past kv_len[b] may be anything.  Scores, maxima and
+ * sums are fp32; the probabilities are rounded to the cache's type before they multiply v.
+ * Deterministic for given inputs, sizes and device.
+ *   workspace: laq_paged_attention_workspace_bytes bytes, 16-byte aligned, ZERO-FILLED before its
+ * first use (a completed call leaves its counters zero).  Word 0 (uint32) is the device-side status:
+ * 0, or LAQ_ERR_TIMEOUT if a wait gave up (out undefined; zero the workspace before the next call).
+ * Calls sharing a workspace must not overlap in time.
+ */
+laq_status laq_paged_attention(const laq_paged_kv *kv, const void *q, int64_t q_stride, int64_t T,
+                               int64_t max_q, int32_t Hq, float scale, void *out, void *workspace,
+                               size_t workspace_bytes, void *stream);
+
+/*
+ * laq_sample -- the next token of each row of logits [M][V] (row m at m * row_stride elements; fp16,
+ * bf16 or fp32, aligned to its type) by a given uniform random number u[m] in [0, 1).
+ *   Row settings, each [M] or NULL (off): temperature t (<= 0 or NaN: the first maximum, whatever u;
+ *   NULL: 1), top_k k (<= 0: off), top_p p (>= 1 or NaN: off), min_p f (<= 0 or NaN: off).
+ *   1. weights: w_v = floor(2^40 * expf((x_v - max x) / t)), 2^40 for the maxima, as whole numbers;
+ *   2. order: by logit, descending, equal ones by index, ascending;
+ *   3. top_k keeps the first k; top_p of those the fewest first ones whose sum reaches
+ *      floor(p * sum of those), at least one; min_p of those the ones with w_v >= floor(f * 2^40);
+ *   4. out[m] is the first index v, in ascending order of the index, at which the sum of the kept
+ *      weights up to v exceeds floor(u * their sum); p_out[m] (fp32, may be NULL) its share of the sum.
+ * p, f and u count in steps of 2^-24 (f of 2^-40); p * sum and u * sum are formed exactly.  The sums
+ * are whole numbers, so that no result depends on the order of a summation: a row's token is the same
+ * in any batch.  NaN logits count as -inf; +inf as the only maxima; a row of nothing else than -inf
+ * gives token 0 with p_out 0.  1 <= V <= 2^22, 0 <= M <= 65535, row_stride >= V.
+ */
+laq_status laq_sample(const void *logits, int32_t dtype, int64_t M, int64_t V, int64_t row_stride,
+                      const float *temperature, const int32_t *top_k, const float *top_p,
+                      const float *min_p, const float *u, int32_t *out, float *p_out, void *stream);
+
+/* ======================================================================================
  * The online pairwise rotation of rotation-based quantizers (the comparison of Sec. 5.2):
  * ParoQuant-style methods turn each projection's input by a transform that cannot be folded
  * into the weights and so runs before every projection at every token (Sec. 1, Sec. 2).  LAQuant

@@ -25,7 +25,8 @@ EXPORTS = ("laq_status_str", "laq_version", "laq_packed_bytes", "laq_quantize_rt
            "laq_attention_decode", "laq_attention_qkv_workspace_bytes", "laq_attention_qkv",
            "laq_silu_mul", "laq_embed", "laq_argmax", "laq_rotation_tables",
            "laq_pairwise_rotate", "laq_pass_plan_sizes", "laq_pass_plan_build",
-           "laq_pass_workspace_bytes", "laq_pass_prepare", "laq_pass_run")
+           "laq_pass_workspace_bytes", "laq_pass_prepare", "laq_pass_run", "laq_paged_append",
+           "laq_paged_attention_workspace_bytes", "laq_paged_attention", "laq_sample")
 CHAIN_MAX = 384  # LAQ_CHAIN_MAX
 
 
@@ -89,6 +90,20 @@ class Gemv(ctypes.Structure):
                 ("wait_prev", ctypes.c_int32)]
 
 
+class PagedKv(ctypes.Structure):
+    """struct laq_paged_kv."""
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("block_table", ctypes.c_void_p),
+                ("q_start", ctypes.c_void_p), ("kv_len", ctypes.c_void_p),
+                ("pages", ctypes.c_int64), ("page_stride", ctypes.c_int64),
+                ("head_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64),
+                ("batch", ctypes.c_int64), ("table_stride", ctypes.c_int64),
+                ("max_pages", ctypes.c_int64), ("page_size", ctypes.c_int32),
+                ("Hkv", ctypes.c_int32), ("D", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+
+F16, BF16, F32 = 0, 1, 2  # LAQ_F16, LAQ_BF16, LAQ_F32
+
+
 @functools.lru_cache(maxsize=1)
 def lib():
     if not os.path.exists(LIB_PATH):
@@ -139,6 +154,12 @@ def lib():
     L.laq_pass_workspace_bytes.restype = SZ
     L.laq_pass_prepare.argtypes = [P, P, SZ, P]
     L.laq_pass_run.argtypes = [P, P, P, SZ, P]
+    KV = ctypes.POINTER(PagedKv)
+    L.laq_paged_append.argtypes = [KV, P, I64, I64, I32, P, P, F, F, P, P]
+    L.laq_paged_attention_workspace_bytes.argtypes = [I64, I64, I64, I32, I32]
+    L.laq_paged_attention_workspace_bytes.restype = SZ
+    L.laq_paged_attention.argtypes = [KV, P, I64, I64, I64, I32, F, P, P, SZ, P]
+    L.laq_sample.argtypes = [P, I32, I64, I64, I64, P, P, P, P, P, P, P, P]
     for name in ("laq_quantize_rtn", "laq_pack", "laq_unpack", "laq_quantize_pack",
                  "laq_gemm_wxg128",
                  "laq_gemm_plan", "laq_gemm_wxg128_config", "laq_gemm_chain",
@@ -147,7 +168,7 @@ def lib():
                  "laq_attention_decode", "laq_attention_qkv", "laq_silu_mul", "laq_embed",
                  "laq_argmax", "laq_rotation_tables", "laq_pairwise_rotate",
                  "laq_pass_plan_sizes", "laq_pass_plan_build", "laq_pass_prepare",
-                 "laq_pass_run"):
+                 "laq_pass_run", "laq_paged_append", "laq_paged_attention", "laq_sample"):
         getattr(L, name).restype = I
     return L
 
@@ -474,6 +495,140 @@ def laq_argmax(logits, out=None, stream=None):
     if out is None:
         out = torch.empty((M,), dtype=torch.int32, device=logits.device)
     _check(lib().laq_argmax(_ptr(logits), M, V, _ptr(out), _stream(stream)), "laq_argmax")
+    return out
+
+
+# ---- a serving step over a paged cache ----
+
+def _dtype(t):
+    import torch
+    try:
+        return {torch.float16: F16, torch.bfloat16: BF16, torch.float32: F32}[t.dtype]
+    except KeyError:
+        raise TypeError(f"fp16, bf16 or fp32 expected, not {t.dtype}") from None
+
+
+def _typed(name, t, dtype, dense=True):
+    """``t`` (a tensor or None) has this dtype and, if ``dense``, no gaps; else TypeError /
+    ValueError: what the C ABI takes as a bare address is checked here."""
+    if t is None:
+        return
+    if t.dtype != dtype:
+        raise TypeError(f"{name}: {dtype} expected, not {t.dtype}")
+    if dense and not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+
+
+def _row_stride(t, width):
+    """Elements between rows; a single row has none to speak of."""
+    return t.stride(0) if t.shape[0] > 1 else width
+
+
+class PagedCache:
+    """A paged cache and the batch that works on it (laq_paged_kv): ``k`` and ``v``
+    [pages, Hkv, page_size, 128] fp16 or bf16, of the same strides (any order of pages, heads and
+    slots, for instance a transposed view of [pages, page_size, Hkv, 128]), ``block_table`` int32
+    [batch, max_pages], ``q_start`` int32 [batch + 1] (request b's new tokens are the rows
+    q_start[b] .. q_start[b + 1] - 1), ``kv_len`` int32 [batch] (cached tokens, the new ones among
+    them).  Holds the tensors; their contents may change from call to call."""
+
+    def __init__(self, k, v, block_table, q_start, kv_len):
+        import torch
+        if k.dim() != 4 or k.shape != v.shape or k.stride() != v.stride() or k.stride(3) != 1:
+            raise ValueError("k and v [pages, Hkv, page_size, D] of equal strides expected")
+        _typed("v", v, k.dtype, dense=False)
+        _typed("block_table", block_table, torch.int32, dense=False)
+        _typed("q_start", q_start, torch.int32)
+        _typed("kv_len", kv_len, torch.int32)
+        batch = kv_len.shape[0]
+        if (q_start.shape != (batch + 1,) or block_table.dim() != 2 or
+                block_table.shape[0] != batch or
+                (block_table.shape[1] > 1 and block_table.stride(1) != 1)):
+            raise ValueError("block_table [batch, max_pages], q_start [batch + 1] expected")
+        pages, Hkv, page_size, D = k.shape
+        self.k, self.v, self.block_table, self.q_start, self.kv_len = (k, v, block_table, q_start,
+                                                                       kv_len)
+        self.Hkv, self.dtype = Hkv, k.dtype
+        self.struct = PagedKv(k.data_ptr(), v.data_ptr(), block_table.data_ptr(),
+                              q_start.data_ptr(), kv_len.data_ptr(), pages, k.stride(0),
+                              k.stride(1), k.stride(2), batch,
+                              _row_stride(block_table, block_table.shape[1]),
+                              block_table.shape[1], page_size, Hkv, D, _dtype(k))
+        self.ref = ctypes.byref(self.struct)
+
+
+def laq_paged_append(qkv, cache, Hq, theta, eps, q_norm_w=None, k_norm_w=None, q_out=None,
+                     stream=None):
+    """qkv [T, (Hq + 2 Hkv) * 128] (rows may be strided) -> q_out [T, Hq, 128]: q and k normalised
+    per head (where weights are given) and rotated, k and v stored in the cache's pages."""
+    T, width = qkv.shape
+    if width != (Hq + 2 * cache.Hkv) * 128 or qkv.stride(1) != 1:
+        raise ValueError("qkv [T, (Hq + 2 Hkv) * 128] expected")
+    for name, t in (("qkv", qkv), ("q_norm_w", q_norm_w), ("k_norm_w", k_norm_w)):
+        _typed(name, t, cache.dtype, dense=t is not qkv)
+    if q_out is None:
+        q_out = qkv.new_empty((T, Hq, 128))
+    else:
+        _typed("q_out", q_out, cache.dtype)
+        if q_out.numel() != T * Hq * 128:
+            raise ValueError("q_out [T, Hq, 128] expected")
+    _check(lib().laq_paged_append(cache.ref, _ptr(qkv), _row_stride(qkv, width), T, Hq,
+                                  _ptr(q_norm_w), _ptr(k_norm_w), theta, eps, _ptr(q_out),
+                                  _stream(stream)), "laq_paged_append")
+    return q_out
+
+
+def paged_attention_workspace(T, batch, max_q, Hq, Hkv, device):
+    """A zero-filled workspace for laq_paged_attention calls of at most these sizes."""
+    import torch
+    n = int(lib().laq_paged_attention_workspace_bytes(T, batch, max_q, Hq, Hkv))
+    if n == 0:
+        raise ValueError("invalid attention sizes")
+    return torch.zeros((n,), dtype=torch.uint8, device=device)
+
+
+def laq_paged_attention(q, cache, max_q, scale, workspace, out=None, stream=None):
+    """out [T, Hq, 128] = causal grouped-query attention of the batch's new tokens q [T, Hq, 128]
+    (rows may be strided) over the paged cache, at most ``max_q`` new tokens per request."""
+    T, Hq, D = q.shape
+    if D != 128 or q.stride(2) != 1 or (Hq > 1 and q.stride(1) != 128):
+        raise ValueError("q [T, Hq, 128] with dense rows expected")
+    _typed("q", q, cache.dtype, dense=False)
+    if out is None:
+        out = q.new_empty((T, Hq, 128))
+    else:
+        _typed("out", out, cache.dtype)
+        if out.numel() != T * Hq * 128:
+            raise ValueError("out [T, Hq, 128] expected")
+    _check(lib().laq_paged_attention(cache.ref, _ptr(q), _row_stride(q, Hq * 128), T, max_q, Hq,
+                                     scale, _ptr(out), _ptr(workspace),
+                                     workspace.numel() * workspace.element_size(),
+                                     _stream(stream)), "laq_paged_attention")
+    return out
+
+
+def laq_sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, out=None,
+               p_out=None, stream=None):
+    """out [M] int32: the next token of each row of logits [M, V] (fp16, bf16 or fp32; rows may be
+    strided) by the uniform random numbers u [M] fp32 in [0, 1).  ``temperature``, ``top_p``,
+    ``min_p`` fp32 [M] and ``top_k`` int32 [M] are per row, None: off.  ``p_out`` fp32 [M], if given,
+    receives each token's probability among the kept ones."""
+    import torch
+    M, V = logits.shape
+    if V > 1 and logits.stride(1) != 1:
+        raise ValueError("logits [M, V] with dense rows expected")
+    if out is None:
+        out = torch.empty((M,), dtype=torch.int32, device=logits.device)
+    f32, i32 = torch.float32, torch.int32
+    for name, t, dt in (("u", u, f32), ("temperature", temperature, f32), ("top_k", top_k, i32),
+                        ("top_p", top_p, f32), ("min_p", min_p, f32), ("out", out, i32),
+                        ("p_out", p_out, f32)):
+        _typed(name, t, dt)
+        if t is not None and t.shape != (M,):
+            raise ValueError(f"{name}: [{M}] expected")
+    _check(lib().laq_sample(_ptr(logits), _dtype(logits), M, V, _row_stride(logits, V),
+                            _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p), _ptr(u),
+                            _ptr(out), _ptr(p_out), _stream(stream)), "laq_sample")
     return out
 
 

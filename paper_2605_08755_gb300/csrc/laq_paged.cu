@@ -1,0 +1,357 @@
+// laq_paged.cu -- the paged cache: host checks, the append of new keys and values with the per-head
+// norms and the rotation, and attention of the new tokens over the pages.
+#include <math.h>
+
+#include "laq_device.cuh"
+#include "laq_paged.cuh"
+
+namespace laq {
+
+laq_status paged_kv(const laq_paged_kv* kv, int64_t T, int32_t Hq, PagedKv* out) {
+    if (!kv || !kv->k || !kv->v || !kv->block_table || !kv->q_start || !kv->kv_len)
+        return LAQ_ERR_NULL;
+    const int64_t lim = (int64_t)1 << 38, most = (int64_t)1 << 24;
+    const int P = kv->page_size;
+    if (kv->D != kPagedDim || kv->Hkv < 1 || kv->Hkv > 4096 || Hq < 1 || Hq % kv->Hkv ||
+        Hq / kv->Hkv > 64 || P < 8 || P > 1024 || (P & (P - 1)) || T < 0 || T > most ||
+        kv->batch < 0 || kv->batch > most || kv->pages < 1 || kv->pages > 0x7fffffff ||
+        kv->max_pages < 1 || kv->max_pages > 0x7fffffff / P || kv->table_stride < kv->max_pages ||
+        kv->token_stride < kPagedDim || kv->head_stride < kPagedDim || kv->page_stride < kPagedDim ||
+        kv->token_stride >= lim || kv->head_stride >= lim || kv->page_stride >= lim ||
+        ((kv->token_stride | kv->head_stride | kv->page_stride) & 7) ||
+        kv->table_stride > (int64_t)1 << 40)
+        return LAQ_ERR_SHAPE;
+    if (kv->dtype != LAQ_F16 && kv->dtype != LAQ_BF16) return LAQ_ERR_CONFIG;
+    if ((((uintptr_t)kv->k | (uintptr_t)kv->v) & 15u) ||
+        (((uintptr_t)kv->block_table | (uintptr_t)kv->q_start | (uintptr_t)kv->kv_len) & 3u))
+        return LAQ_ERR_ALIGN;
+    PagedKv o = {};
+    o.k = static_cast<uint16_t*>(kv->k);
+    o.v = static_cast<uint16_t*>(kv->v);
+    o.table = kv->block_table;
+    o.q_start = kv->q_start;
+    o.kv_len = kv->kv_len;
+    o.pages = kv->pages;
+    o.page_stride = kv->page_stride;
+    o.head_stride = kv->head_stride;
+    o.token_stride = kv->token_stride;
+    o.table_stride = kv->table_stride;
+    o.batch = (int32_t)kv->batch;
+    o.max_tokens = (int32_t)(kv->max_pages * P);
+    o.page_bits = __builtin_ctz((unsigned)P);
+    o.Hkv = kv->Hkv;
+    *out = o;
+    return LAQ_OK;
+}
+
+namespace {
+
+// ---- append ----
+// One half-warp per head vector: lane l of 16 holds elements 4l .. 4l+3 and 64 + 4l .. 64 + 4l+3, the
+// two sides of four rotation pairs, so the norm is four shuffles and the rotation none.  A CTA takes
+// kTokens tokens (or some of the heads of one token, where there are few): one warp finds each token's request, position
+// and slot, one thread turns each (token, frequency), then the half-warps walk the CTA's head vectors,
+// kAhead of them loaded before anything waits.
+//   The angle p * theta^(-2i/D) is reduced in whole turns first: turn[i] = theta^(-2i/D) / 2 pi as a
+// 64-bit fraction, so p * turn[i] mod 2^64 is the fraction of a turn to 2^-64 p, whatever p (an fp32
+// product is off by 2^-24 of the angle: 2e-3 radians at position 40,000).
+//   Bound: HBM (each head vector read and written once); for few tokens the chain request -> length ->
+// page -> store, about four dependent loads.
+constexpr int kAppendThreads = 256;
+constexpr int kAhead = 4;
+
+struct AppendParams {
+    PagedKv kv;
+    const uint16_t* qkv;
+    const uint16_t *qw, *kw;
+    uint16_t* q_out;
+    int64_t qkv_stride;
+    int T, Hq, tokens, heads_per_cta;
+    float eps;
+    uint64_t turn[kPagedDim / 2];
+};
+
+template <bool BF>
+__global__ void __launch_bounds__(kAppendThreads) paged_append_kernel(
+    const __grid_constant__ AppendParams p) {
+    using H = Half16<BF>;
+    constexpr int kTok = 4;
+    __shared__ float4 cs[kTok][kPagedDim / 8], sn[kTok][kPagedDim / 8];
+    __shared__ int pos_s[kTok];        // position
+    __shared__ int64_t slot_s[kTok];   // element offset of the slot (head 0), -1: none; -2: no request
+    pdl_launch_dependents();
+    pdl_wait();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int t0 = blockIdx.x * p.tokens, nt = min(p.tokens, p.T - t0);
+    const int nh = p.Hq + 2 * p.kv.Hkv, h0 = blockIdx.y * p.heads_per_cta;
+    const int heads = min(p.heads_per_cta, nh - h0), rows = nt * heads;
+    const int hw = threadIdx.x >> 4, l = threadIdx.x & 15;
+    constexpr int kStride = kAppendThreads / 16;
+    uint2 lo[kAhead], hi[kAhead];
+    auto load = [&](int r0) {
+#pragma unroll
+        for (int a = 0; a < kAhead; ++a) {
+            const int r = r0 + a * kStride;
+            if (r < rows) {
+                const uint16_t* src = p.qkv + (int64_t)(t0 + r / heads) * p.qkv_stride +
+                                      (int64_t)(h0 + r % heads) * kPagedDim + 4 * l;
+                lo[a] = *reinterpret_cast<const uint2*>(src);
+                hi[a] = *reinterpret_cast<const uint2*>(src + 64);
+            }
+        }
+    };
+    load(hw);
+    if (warp < nt) {
+        const int t = t0 + warp, b = request_of(p.kv.q_start, p.kv.batch, t);
+        const int s0 = b < p.kv.batch ? p.kv.q_start[b] : 0x7fffffff;
+        int64_t slot = -2;
+        int pos = 0;
+        if (s0 >= 0 && t >= s0) {
+            const int n = p.kv.q_start[b + 1] - s0;
+            const int len = min(max(p.kv.kv_len[b], 0), p.kv.max_tokens);
+            pos = len - n + (t - s0);
+            slot = -1;
+            if (pos >= 0) {
+                const int64_t page =
+                    p.kv.table[(int64_t)b * p.kv.table_stride + (pos >> p.kv.page_bits)];
+                if (page >= 0 && page < p.kv.pages)
+                    slot = page * p.kv.page_stride +
+                           (int64_t)(pos & ((1 << p.kv.page_bits) - 1)) * p.kv.token_stride;
+            }
+        }
+        if (lane == 0) {
+            pos_s[warp] = pos;
+            slot_s[warp] = slot;
+        }
+    }
+    __syncthreads();
+    if ((int)threadIdx.x < nt * (kPagedDim / 2)) {
+        const int i = threadIdx.x & 63, t = threadIdx.x >> 6;
+        const uint64_t f = (uint64_t)(int64_t)pos_s[t] * p.turn[i];
+        const float half_turns = (float)(int32_t)(f >> 32) * 0x1p-31f;  // in [-1, 1)
+        float s, c;
+        sincospif(half_turns, &s, &c);
+        reinterpret_cast<float*>(cs[t])[i] = c;
+        reinterpret_cast<float*>(sn[t])[i] = s;
+    }
+    float wq[8], wk[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) wq[e] = wk[e] = 1.f;
+    auto weights = [&](const uint16_t* w, float (&o)[8]) {
+        if (!w) return;
+#pragma unroll
+        for (int side = 0; side < 2; ++side) {
+            const uint2 u = *reinterpret_cast<const uint2*>(w + 64 * side + 4 * l);
+            const float2 a = H::unpack(u.x), b = H::unpack(u.y);
+            o[4 * side] = a.x; o[4 * side + 1] = a.y; o[4 * side + 2] = b.x; o[4 * side + 3] = b.y;
+        }
+    };
+    weights(p.qw, wq);
+    weights(p.kw, wk);
+    __syncthreads();
+    for (int r0 = hw; r0 < rows; r0 += kAhead * kStride) {
+        if (r0 != hw) load(r0);
+#pragma unroll
+        for (int a = 0; a < kAhead; ++a) {
+            const int r = r0 + a * kStride;
+            // (the lanes of a half-warp leave together; the other half may stay: the shuffles below
+            // name the half's own lanes)
+            if (r >= rows) break;
+            const int t = r / heads, h = h0 + r % heads;
+            const int64_t slot = slot_s[t];
+            if (slot == -2) continue;
+            const bool is_q = h < p.Hq, is_v = h >= p.Hq + p.kv.Hkv;
+            uint2 ol = lo[a], oh = hi[a];
+            if (!is_v) {
+                float x[8];
+                const float2 f0 = H::unpack(lo[a].x), f1 = H::unpack(lo[a].y),
+                             f2 = H::unpack(hi[a].x), f3 = H::unpack(hi[a].y);
+                x[0] = f0.x; x[1] = f0.y; x[2] = f1.x; x[3] = f1.y;
+                x[4] = f2.x; x[5] = f2.y; x[6] = f3.x; x[7] = f3.y;
+                if (is_q ? p.qw != nullptr : p.kw != nullptr) {
+                    float ss = 0.f;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) ss = fmaf(x[e], x[e], ss);
+                    const unsigned half = 0xffffu << (threadIdx.x & 16);
+#pragma unroll
+                    for (int o = 8; o > 0; o >>= 1) ss += __shfl_xor_sync(half, ss, o);
+                    const float inv = rsqrtf(ss / (float)kPagedDim + p.eps);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[e] = x[e] * inv * (is_q ? wq[e] : wk[e]);
+                }
+                const float4 c4 = cs[t][l], s4 = sn[t][l];
+                const float c[4] = {c4.x, c4.y, c4.z, c4.w}, s[4] = {s4.x, s4.y, s4.z, s4.w};
+                float y[8];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    y[e] = x[e] * c[e] - x[4 + e] * s[e];
+                    y[4 + e] = x[4 + e] * c[e] + x[e] * s[e];
+                }
+                ol = make_uint2(H::pack(y[0], y[1]), H::pack(y[2], y[3]));
+                oh = make_uint2(H::pack(y[4], y[5]), H::pack(y[6], y[7]));
+            }
+            uint16_t* dst;
+            if (is_q) {
+                dst = p.q_out + ((int64_t)(t0 + t) * p.Hq + h) * kPagedDim;
+            } else {
+                if (slot < 0) continue;
+                const int g = h - p.Hq - (is_v ? p.kv.Hkv : 0);
+                dst = (is_v ? p.kv.v : p.kv.k) + slot + (int64_t)g * p.kv.head_stride;
+            }
+            *reinterpret_cast<uint2*>(dst + 4 * l) = ol;
+            *reinterpret_cast<uint2*>(dst + 64 + 4 * l) = oh;
+        }
+    }
+}
+
+// ---- attention: one warp per (row, q head), the running maximum and sum of the softmax ----
+struct AttnRowParams {
+    PagedKv kv;
+    const uint16_t* q;
+    uint16_t* out;
+    int64_t q_stride;
+    int T, Hq, max_q;
+    float scale_log2;
+};
+
+template <bool BF>
+__global__ void __launch_bounds__(128) paged_attn_row_kernel(const __grid_constant__ AttnRowParams p) {
+    using H = Half16<BF>;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int h = blockIdx.y * 4 + warp, t = blockIdx.x;
+    if (h >= p.Hq) return;
+    const int b = request_of(p.kv.q_start, p.kv.batch, t);
+    if (b >= p.kv.batch) return;
+    const int s0 = p.kv.q_start[b];
+    if (s0 < 0 || t < s0 || t - s0 >= p.max_q) return;
+    const int len = min(max(p.kv.kv_len[b], 0), p.kv.max_tokens);
+    const int pos = len - (p.kv.q_start[b + 1] - s0) + (t - s0);
+    const int64_t g = h / (p.Hq / p.kv.Hkv);
+    const uint2 qr = *reinterpret_cast<const uint2*>(p.q + (int64_t)t * p.q_stride +
+                                                     h * kPagedDim + 4 * lane);
+    const float2 q0 = H::unpack(qr.x), q1 = H::unpack(qr.y);
+    float m = -INFINITY, sum = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i <= pos; ++i) {
+        const int64_t page = p.kv.table[(int64_t)b * p.kv.table_stride + (i >> p.kv.page_bits)];
+        uint2 kr = make_uint2(0u, 0u), vr = make_uint2(0u, 0u);
+        if (page >= 0 && page < p.kv.pages) {
+            const int64_t off = page * p.kv.page_stride + g * p.kv.head_stride +
+                                (int64_t)(i & ((1 << p.kv.page_bits) - 1)) * p.kv.token_stride +
+                                4 * lane;
+            kr = *reinterpret_cast<const uint2*>(p.kv.k + off);
+            vr = *reinterpret_cast<const uint2*>(p.kv.v + off);
+        }
+        const float2 k0 = H::unpack(kr.x), k1 = H::unpack(kr.y);
+        float s = q0.x * k0.x + q0.y * k0.y + q1.x * k1.x + q1.y * k1.y;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+        s *= p.scale_log2;
+        const float mn = fmaxf(m, s), f = m == -INFINITY ? 0.f : exp2f(m - mn),
+                    e = exp2f(s - mn);
+        m = mn;
+        sum = sum * f + e;
+        const float2 v0 = H::unpack(vr.x), v1 = H::unpack(vr.y);
+        acc[0] = acc[0] * f + e * v0.x;
+        acc[1] = acc[1] * f + e * v0.y;
+        acc[2] = acc[2] * f + e * v1.x;
+        acc[3] = acc[3] * f + e * v1.y;
+    }
+    const float inv = pos >= 0 ? 1.f / sum : 0.f;
+    *reinterpret_cast<uint2*>(p.out + ((int64_t)t * p.Hq + h) * kPagedDim + 4 * lane) =
+        make_uint2(H::pack(acc[0] * inv, acc[1] * inv), H::pack(acc[2] * inv, acc[3] * inv));
+}
+
+template <typename P>
+laq_status launch_paged(void (*fn)(P), dim3 grid, int threads, void* stream, const P& p) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.stream = static_cast<cudaStream_t>(stream);
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, fn, p) == cudaSuccess ? LAQ_OK : LAQ_ERR_CUDA;
+}
+
+}  // namespace
+}  // namespace laq
+
+using namespace laq;
+
+extern "C" {
+
+laq_status laq_paged_append(const laq_paged_kv* kv, const void* qkv, int64_t qkv_stride, int64_t T,
+                            int32_t Hq, const void* q_norm_w, const void* k_norm_w, float theta,
+                            float eps, void* q_out, void* stream) {
+    AppendParams p = {};
+    const laq_status st = paged_kv(kv, T, Hq, &p.kv);
+    if (st != LAQ_OK) return st;
+    if (!qkv || !q_out) return LAQ_ERR_NULL;
+    const int nh = Hq + 2 * kv->Hkv;
+    if (qkv_stride < (int64_t)nh * kPagedDim || qkv_stride > (int64_t)1 << 38 || (qkv_stride & 3) ||
+        !(theta > 1.f) || !isfinite(theta) || !(eps >= 0.f))
+        return LAQ_ERR_SHAPE;
+    if (((uintptr_t)qkv | (uintptr_t)q_out | (uintptr_t)q_norm_w | (uintptr_t)k_norm_w) & 7u)
+        return LAQ_ERR_ALIGN;
+    if (T == 0 || kv->batch == 0) return LAQ_OK;
+    p.qkv = static_cast<const uint16_t*>(qkv);
+    p.qw = static_cast<const uint16_t*>(q_norm_w);
+    p.kw = static_cast<const uint16_t*>(k_norm_w);
+    p.q_out = static_cast<uint16_t*>(q_out);
+    p.qkv_stride = qkv_stride;
+    p.T = (int)T;
+    p.Hq = Hq;
+    p.eps = eps;
+    // turns per position of every frequency, from one power and products (64 steps of 2^-53)
+    const double ratio = pow((double)theta, -2.0 / kPagedDim);
+    double f = 0.15915494309189533577 * 0x1p64;  // 2^64 / (2 pi)
+    for (int i = 0; i < kPagedDim / 2; ++i, f *= ratio) p.turn[i] = (uint64_t)f;
+    p.tokens = 4;
+    p.heads_per_cta = nh;
+    const dim3 grid((unsigned)((T + p.tokens - 1) / p.tokens),
+                    (unsigned)((nh + p.heads_per_cta - 1) / p.heads_per_cta));
+    return kv->dtype == LAQ_BF16
+               ? launch_paged(paged_append_kernel<true>, grid, kAppendThreads, stream, p)
+               : launch_paged(paged_append_kernel<false>, grid, kAppendThreads, stream, p);
+}
+
+size_t laq_paged_attention_workspace_bytes(int64_t T, int64_t batch, int64_t max_q, int32_t Hq,
+                                           int32_t Hkv) {
+    const int64_t most = (int64_t)1 << 24;
+    if (T < 0 || batch < 0 || max_q < 0 || T > most || batch > most || Hq < 1 || Hkv < 1 ||
+        Hkv > 4096 || Hq % Hkv || Hq / Hkv > 64)
+        return 0;
+    return 256;
+}
+
+laq_status laq_paged_attention(const laq_paged_kv* kv, const void* q, int64_t q_stride, int64_t T,
+                               int64_t max_q, int32_t Hq, float scale, void* out, void* workspace,
+                               size_t workspace_bytes, void* stream) {
+    AttnRowParams p = {};
+    const laq_status st = paged_kv(kv, T, Hq, &p.kv);
+    if (st != LAQ_OK) return st;
+    if (!q || !out || !workspace) return LAQ_ERR_NULL;
+    if (q_stride < (int64_t)Hq * kPagedDim || q_stride > (int64_t)1 << 38 || (q_stride & 7) ||
+        max_q < 0 || !(scale > 0.f) || !isfinite(scale))
+        return LAQ_ERR_SHAPE;
+    if (((uintptr_t)q | (uintptr_t)out) & 15u) return LAQ_ERR_ALIGN;
+    if (((uintptr_t)workspace & 15u) ||
+        workspace_bytes < laq_paged_attention_workspace_bytes(T, kv->batch, max_q, Hq, kv->Hkv))
+        return LAQ_ERR_WORKSPACE;
+    if (T == 0 || kv->batch == 0 || max_q == 0) return LAQ_OK;
+    p.q = static_cast<const uint16_t*>(q);
+    p.out = static_cast<uint16_t*>(out);
+    p.q_stride = q_stride;
+    p.T = (int)T;
+    p.Hq = Hq;
+    p.max_q = (int)(max_q < T ? max_q : T);
+    p.scale_log2 = scale * 1.44269504088896340736f;
+    const dim3 grid((unsigned)T, (unsigned)((Hq + 3) / 4));
+    return kv->dtype == LAQ_BF16
+               ? launch_paged(paged_attn_row_kernel<true>, grid, 128, stream, p)
+               : launch_paged(paged_attn_row_kernel<false>, grid, 128, stream, p);
+}
+
+}  // extern "C"
