@@ -1,9 +1,10 @@
 // laq_paged.cu -- the paged cache: host checks, the append of new keys and values with the per-head
-// norms and the rotation, and attention of the new tokens over the pages.
+// norms and the rotation, and the entry points of the attention over the pages.
 #include <math.h>
 
 #include "laq_device.cuh"
 #include "laq_paged.cuh"
+#include "laq_paged_attn.cuh"
 
 namespace laq {
 
@@ -204,63 +205,6 @@ __global__ void __launch_bounds__(kAppendThreads) paged_append_kernel(
     }
 }
 
-// ---- attention: one warp per (row, q head), the running maximum and sum of the softmax ----
-struct AttnRowParams {
-    PagedKv kv;
-    const uint16_t* q;
-    uint16_t* out;
-    int64_t q_stride;
-    int T, Hq, max_q;
-    float scale_log2;
-};
-
-template <bool BF>
-__global__ void __launch_bounds__(128) paged_attn_row_kernel(const __grid_constant__ AttnRowParams p) {
-    using H = Half16<BF>;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int h = blockIdx.y * 4 + warp, t = blockIdx.x;
-    if (h >= p.Hq) return;
-    const int b = request_of(p.kv.q_start, p.kv.batch, t);
-    if (b >= p.kv.batch) return;
-    const int s0 = p.kv.q_start[b];
-    if (s0 < 0 || t < s0 || t - s0 >= p.max_q) return;
-    const int len = min(max(p.kv.kv_len[b], 0), p.kv.max_tokens);
-    const int pos = len - (p.kv.q_start[b + 1] - s0) + (t - s0);
-    const int64_t g = h / (p.Hq / p.kv.Hkv);
-    const uint2 qr = *reinterpret_cast<const uint2*>(p.q + (int64_t)t * p.q_stride +
-                                                     h * kPagedDim + 4 * lane);
-    const float2 q0 = H::unpack(qr.x), q1 = H::unpack(qr.y);
-    float m = -INFINITY, sum = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int i = 0; i <= pos; ++i) {
-        const int64_t page = p.kv.table[(int64_t)b * p.kv.table_stride + (i >> p.kv.page_bits)];
-        uint2 kr = make_uint2(0u, 0u), vr = make_uint2(0u, 0u);
-        if (page >= 0 && page < p.kv.pages) {
-            const int64_t off = page * p.kv.page_stride + g * p.kv.head_stride +
-                                (int64_t)(i & ((1 << p.kv.page_bits) - 1)) * p.kv.token_stride +
-                                4 * lane;
-            kr = *reinterpret_cast<const uint2*>(p.kv.k + off);
-            vr = *reinterpret_cast<const uint2*>(p.kv.v + off);
-        }
-        const float2 k0 = H::unpack(kr.x), k1 = H::unpack(kr.y);
-        float s = q0.x * k0.x + q0.y * k0.y + q1.x * k1.x + q1.y * k1.y;
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-        s *= p.scale_log2;
-        const float mn = fmaxf(m, s), f = m == -INFINITY ? 0.f : exp2f(m - mn),
-                    e = exp2f(s - mn);
-        m = mn;
-        sum = sum * f + e;
-        const float2 v0 = H::unpack(vr.x), v1 = H::unpack(vr.y);
-        acc[0] = acc[0] * f + e * v0.x;
-        acc[1] = acc[1] * f + e * v0.y;
-        acc[2] = acc[2] * f + e * v1.x;
-        acc[3] = acc[3] * f + e * v1.y;
-    }
-    const float inv = pos >= 0 ? 1.f / sum : 0.f;
-    *reinterpret_cast<uint2*>(p.out + ((int64_t)t * p.Hq + h) * kPagedDim + 4 * lane) =
-        make_uint2(H::pack(acc[0] * inv, acc[1] * inv), H::pack(acc[2] * inv, acc[3] * inv));
-}
-
 template <typename P>
 laq_status launch_paged(void (*fn)(P), dim3 grid, int threads, void* stream, const P& p) {
     cudaLaunchConfig_t cfg = {};
@@ -323,14 +267,14 @@ size_t laq_paged_attention_workspace_bytes(int64_t T, int64_t batch, int64_t max
     if (T < 0 || batch < 0 || max_q < 0 || T > most || batch > most || Hq < 1 || Hkv < 1 ||
         Hkv > 4096 || Hq % Hkv || Hq / Hkv > 64)
         return 0;
-    return 256;
+    return chunk_workspace_bytes(max_q, Hq / Hkv);
 }
 
 laq_status laq_paged_attention(const laq_paged_kv* kv, const void* q, int64_t q_stride, int64_t T,
                                int64_t max_q, int32_t Hq, float scale, void* out, void* workspace,
                                size_t workspace_bytes, void* stream) {
-    AttnRowParams p = {};
-    const laq_status st = paged_kv(kv, T, Hq, &p.kv);
+    PagedKv o;
+    const laq_status st = paged_kv(kv, T, Hq, &o);
     if (st != LAQ_OK) return st;
     if (!q || !out || !workspace) return LAQ_ERR_NULL;
     if (q_stride < (int64_t)Hq * kPagedDim || q_stride > (int64_t)1 << 38 || (q_stride & 7) ||
@@ -341,17 +285,8 @@ laq_status laq_paged_attention(const laq_paged_kv* kv, const void* q, int64_t q_
         workspace_bytes < laq_paged_attention_workspace_bytes(T, kv->batch, max_q, Hq, kv->Hkv))
         return LAQ_ERR_WORKSPACE;
     if (T == 0 || kv->batch == 0 || max_q == 0) return LAQ_OK;
-    p.q = static_cast<const uint16_t*>(q);
-    p.out = static_cast<uint16_t*>(out);
-    p.q_stride = q_stride;
-    p.T = (int)T;
-    p.Hq = Hq;
-    p.max_q = (int)(max_q < T ? max_q : T);
-    p.scale_log2 = scale * 1.44269504088896340736f;
-    const dim3 grid((unsigned)T, (unsigned)((Hq + 3) / 4));
-    return kv->dtype == LAQ_BF16
-               ? launch_paged(paged_attn_row_kernel<true>, grid, 128, stream, p)
-               : launch_paged(paged_attn_row_kernel<false>, grid, 128, stream, p);
+    return launch_chunk(o, kv->dtype == LAQ_BF16, q, q_stride, (int)T, (int)(max_q < T ? max_q : T),
+                        Hq, scale, out, workspace, static_cast<cudaStream_t>(stream));
 }
 
 }  // extern "C"

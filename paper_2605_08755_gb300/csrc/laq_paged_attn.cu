@@ -1,0 +1,929 @@
+// laq_paged_attn.cu -- attention of chunks of new tokens over the paged cache on the 5th-generation
+// tensor cores.
+//
+// An item is (request, kv head, up to 2 tau of the request's new tokens), tau = 128 / G tokens of G =
+// Hq / Hkv q heads being one tile of up to 128 rows.  Per tile of 128 cached tokens:
+//   S_i = Q_i K^T   (tcgen05.mma, M = N = 128, K = 128; both from shared memory, S in tensor memory)
+//   P_i = 2^(c S_i - c m_i + offset), rounded to the cache's type, over S_i in tensor memory
+//   O_i += P_i V    (P from tensor memory, V from shared memory as it lies: [token][d])
+// for the item's two q tiles i = 0, 1, one warpgroup each, so that one tile's exponentials run while
+// the tensor cores work on the other's products.  An item of one q tile gives the two warpgroups the
+// even and the odd tiles of tokens instead and adds the two results at its end.
+//   m_i is the running maximum, moved only when a row's has grown by more than 2^8 since (the sums
+// and O are in units of 2^(c m_i); a P of up to 2^8 more costs nothing in a floating-point type):
+// then the warp rescales its rows of O.  The offset of 2^7 keeps small fp16 P above the subnormals.
+//   K, V and Q come by TMA in the 128-byte swizzle that the products read; pages that end inside a
+// tile are filled by boxes of a page each.  Rows of V past the request's last token are zeroed in
+// shared memory, since 0 * NaN would not vanish in the product.
+//
+// Work split: one CTA per SM walks an equal share of all items' tiles in order (a "unit" is a tile
+// of 128 tokens of an item, and one more unit for each item's start); an item that a share's border
+// cuts is finished by its CTAs together: each writes its part's O, maximum and sum to the workspace,
+// and when all of them are there each adds up a share of the rows, in the order of the parts.
+#include <cuda.h>
+#include <math.h>
+
+#include <atomic>
+
+#include "laq_device.cuh"
+#include "laq_internal.cuh"
+#include "laq_paged.cuh"
+#include "laq_paged_attn.cuh"
+
+namespace laq {
+namespace {
+
+constexpr int kTile = 128;              // tokens of a K / V tile, rows of a q tile
+constexpr int kHalf = kTile * 128;      // bytes of 64 columns of a tile: rows of 128 bytes
+constexpr int kTileBytes = 2 * kHalf;
+constexpr int kStages = 5;              // K and V tiles in flight (160 KB)
+constexpr int kThreads = 320;           // 2 warpgroups of softmax, a TMA warp, an MMA warp
+constexpr int kSmemTiles = (2 + kStages) * kTileBytes;
+constexpr long long kWaitCycles = 2000000000;  // about a second
+constexpr float kGrow = 8.f;            // how far a maximum may grow before O is rescaled (log2)
+
+struct Bars {
+    uint64_t full[kStages], empty[kStages], q_full, q_empty, v_tail, drain;
+    uint64_t s_full[2], p_full[2], o_full[2], soft;
+    uint32_t tmem, abort;
+    int b, g, t, off;                   // where this CTA's share starts
+    long long left, U, W;
+    int ctas;
+    long long scan[kThreads / 32];
+};
+constexpr int kSmem = kSmemTiles + 1024 + (int)sizeof(Bars);
+
+__device__ __forceinline__ uint32_t s32(const void* p) {
+    return (uint32_t)__cvta_generic_to_shared(p);
+}
+__device__ __forceinline__ void bar_init(uint64_t* b, int n) {
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(s32(b)), "r"(n) : "memory");
+}
+__device__ __forceinline__ void bar_arrive(uint64_t* b) {
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(s32(b)) : "memory");
+}
+__device__ __forceinline__ void bar_expect(uint64_t* b, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(s32(b)), "r"(bytes)
+                 : "memory");
+}
+__device__ __forceinline__ bool bar_try(uint64_t* b, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n"
+        "selp.u32 %0, 1, 0, p;\n}\n"
+        : "=r"(ok)
+        : "r"(s32(b)), "r"(parity)
+        : "memory");
+    return ok;
+}
+// Bounded wait; false once any wait of the CTA has run out (every role then leaves its loop).
+__device__ __forceinline__ bool bar_wait(Bars* s, uint64_t* b, uint32_t parity) {
+    if (bar_try(b, parity)) return true;
+    const long long t0 = clock64();
+    do {
+        if (bar_try(b, parity)) return true;
+        if (*(volatile uint32_t*)&s->abort) return false;
+    } while (clock64() - t0 < kWaitCycles);
+    *(volatile uint32_t*)&s->abort = 1;
+    return false;
+}
+// The same for a whole warp, which stays together.
+__device__ __forceinline__ bool warp_wait(Bars* s, uint64_t* b, uint32_t parity) {
+    return __all_sync(0xffffffffu, bar_wait(s, b, parity));
+}
+// For what is in flight when a wait has run out.
+__device__ __forceinline__ void drain(uint64_t* b, uint32_t parity) {
+    const long long t0 = clock64();
+    while (!bar_try(b, parity) && clock64() - t0 < kWaitCycles) {
+    }
+}
+__device__ __forceinline__ void tma4(uint32_t dst, const CUtensorMap* m, int c0, int c1, int c2,
+                                     int c3, uint64_t* bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], "
+        "[%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
+        "l"(m), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(s32(bar))
+        : "memory");
+}
+__device__ __forceinline__ void tma3(uint32_t dst, const CUtensorMap* m, int c0, int c1, int c2,
+                                     uint64_t* bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], "
+        "[%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+        "l"(m), "r"(c0), "r"(c1), "r"(c2), "r"(s32(bar))
+        : "memory");
+}
+// Shared-memory operand descriptors, 128-byte swizzle (version 1, layout 2): rows of 128 bytes, eight
+// rows 1024 bytes apart.  kdesc: the row is M or N, its 64 columns are K.  vdesc: the row is K, its 64
+// columns N; the next 64 columns of N are kHalf on.
+__device__ __forceinline__ uint64_t kdesc(uint32_t a) {
+    return (uint64_t)((a >> 4) & 0x3fff) | 1ull << 16 | 64ull << 32 | 1ull << 46 | 2ull << 61;
+}
+__device__ __forceinline__ uint64_t vdesc(uint32_t a) {
+    return (uint64_t)((a >> 4) & 0x3fff) | (uint64_t)(kHalf >> 4) << 16 | 64ull << 32 |
+           1ull << 46 | 2ull << 61;
+}
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, int acc) {
+    asm volatile(
+        "{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\n"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(acc)
+        : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, int acc) {
+    asm volatile(
+        "{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\n"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n" ::"r"(d),
+        "r"(a), "l"(b), "r"(idesc), "r"(acc)
+        : "memory");
+}
+__device__ __forceinline__ void commit(uint64_t* b) {
+    asm volatile(
+        "tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(s32(b))
+        : "memory");
+}
+__device__ __forceinline__ void tc_before() {
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+}
+__device__ __forceinline__ void tc_after() {
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+}
+// 32 columns of the warp's 32 lanes of tensor memory, one lane a thread
+__device__ __forceinline__ void tm_ld32(uint32_t a, float* r) {
+    uint32_t* u = reinterpret_cast<uint32_t*>(r);
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,"
+        "%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+        : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]),
+          "=r"(u[7]), "=r"(u[8]), "=r"(u[9]), "=r"(u[10]), "=r"(u[11]), "=r"(u[12]), "=r"(u[13]),
+          "=r"(u[14]), "=r"(u[15]), "=r"(u[16]), "=r"(u[17]), "=r"(u[18]), "=r"(u[19]),
+          "=r"(u[20]), "=r"(u[21]), "=r"(u[22]), "=r"(u[23]), "=r"(u[24]), "=r"(u[25]),
+          "=r"(u[26]), "=r"(u[27]), "=r"(u[28]), "=r"(u[29]), "=r"(u[30]), "=r"(u[31])
+        : "r"(a));
+}
+__device__ __forceinline__ void tm_st32(uint32_t a, const uint32_t* u) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,"
+        "%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};" ::"r"(u[0]),
+        "r"(u[1]), "r"(u[2]), "r"(u[3]), "r"(u[4]), "r"(u[5]), "r"(u[6]), "r"(u[7]), "r"(u[8]),
+        "r"(u[9]), "r"(u[10]), "r"(u[11]), "r"(u[12]), "r"(u[13]), "r"(u[14]), "r"(u[15]),
+        "r"(u[16]), "r"(u[17]), "r"(u[18]), "r"(u[19]), "r"(u[20]), "r"(u[21]), "r"(u[22]),
+        "r"(u[23]), "r"(u[24]), "r"(u[25]), "r"(u[26]), "r"(u[27]), "r"(u[28]), "r"(u[29]),
+        "r"(u[30]), "r"(u[31]), "r"(a)
+        : "memory");
+}
+__device__ __forceinline__ void tm_wait_ld() {
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tm_wait_st() {
+    asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// Pins loaded values behind the wait that makes them valid.
+__device__ __forceinline__ void pin32(float* r) {
+    asm volatile("" : "+f"(r[0]), "+f"(r[1]), "+f"(r[2]), "+f"(r[3]), "+f"(r[4]), "+f"(r[5]),
+                 "+f"(r[6]), "+f"(r[7]), "+f"(r[8]), "+f"(r[9]), "+f"(r[10]), "+f"(r[11]),
+                 "+f"(r[12]), "+f"(r[13]), "+f"(r[14]), "+f"(r[15]));
+    asm volatile("" : "+f"(r[16]), "+f"(r[17]), "+f"(r[18]), "+f"(r[19]), "+f"(r[20]),
+                 "+f"(r[21]), "+f"(r[22]), "+f"(r[23]), "+f"(r[24]), "+f"(r[25]), "+f"(r[26]),
+                 "+f"(r[27]), "+f"(r[28]), "+f"(r[29]), "+f"(r[30]), "+f"(r[31]));
+}
+// The two softmax warpgroups meet (bounded, as every wait); n: meetings before this one.
+__device__ __forceinline__ bool meet(Bars* s, uint32_t& n) {
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) bar_arrive(&s->soft);
+    return warp_wait(s, &s->soft, n++ & 1);
+}
+
+// ---- the walk over the items ----
+// One request: its rows, its tokens before the first new one, its items per kv head.
+struct Req {
+    int s0, n, past, len, m;
+    __device__ void load(const ChunkParams& p, int b) {
+        s0 = p.kv.q_start[b];
+        const int all = p.kv.q_start[b + 1] - s0;
+        len = min(max(p.kv.kv_len[b], 0), p.kv.max_tokens);
+        past = len - all;
+        n = s0 < 0 || s0 >= p.T || all <= 0 ? 0 : min(min(all, p.max_q), p.T - s0);
+        m = (n + 2 * p.tau - 1) / (2 * p.tau);
+    }
+    __device__ int tiles(const ChunkParams& p, int t) const {
+        const int end = past + min(n, (t + 1) * 2 * p.tau);
+        return (max(end, 0) + kTile - 1) / kTile;
+    }
+    // tiles of the first x items (x < m): sum of ceil(max(0, past + (t + 1) 2 tau) / 128), as a sum of
+    // floors of a line, by Euclid's algorithm
+    __device__ long long tiles_before(const ChunkParams& p, int x) const {
+        const int S = 2 * p.tau;
+        const int skip = past < 0 ? min(x, (int)(-(long long)past / S)) : 0;
+        long long sum = 0, n_ = x - skip, M = kTile, a = S,
+                  b = (long long)past + (skip + 1LL) * S + kTile - 1;
+        while (n_ > 0) {
+            sum += n_ * (n_ - 1) / 2 * (a / M) + n_ * (b / M);
+            a %= M;
+            b %= M;
+            const long long y = a * n_ + b;
+            if (y < M) break;
+            n_ = y / M;
+            b = y % M;
+            const long long s = M;
+            M = a;
+            a = s;
+        }
+        return sum;
+    }
+    // units of all items of one kv head
+    __device__ long long units(const ChunkParams& p) const {
+        return m == 0 ? 0 : m + tiles_before(p, m - 1) + tiles(p, m - 1);
+    }
+};
+
+// The part of an item that one CTA works on: tiles lo .. hi - 1 of nt.
+struct Piece {
+    int b, g, row0, ntok, pos0, len, nt, lo, hi;
+    long long U;  // the item's first unit
+    __device__ bool whole() const { return lo == 0 && hi == nt; }
+};
+
+struct Walk {
+    const ChunkParams& p;
+    long long left, U;
+    int b, g, t, off;
+    Req r;
+    __device__ Walk(const ChunkParams& p_, const Bars* s)
+        : p(p_), left(s->left), U(s->U), b(s->b), g(s->g), t(s->t), off(s->off) {
+        if (left > 0) r.load(p, b);
+    }
+    __device__ bool next(Piece& x) {
+        while (left > 0) {
+            const int nt = r.tiles(p, t), units = nt + 1;
+            const int take = (int)min(left, (long long)(units - off));
+            x.b = b;
+            x.g = g;
+            x.row0 = r.s0 + t * 2 * p.tau;
+            x.ntok = min(r.n - t * 2 * p.tau, 2 * p.tau);
+            x.pos0 = r.past + t * 2 * p.tau;
+            x.len = r.len;
+            x.nt = nt;
+            x.lo = max(off - 1, 0);
+            x.hi = off + take - 1;
+            x.U = U;
+            left -= take;
+            if (off + take == units) {
+                off = 0;
+                U += units;
+                if (++t == r.m) {
+                    t = 0;
+                    if (++g == p.kv.Hkv) {
+                        g = 0;
+                        do {
+                            if (++b >= p.kv.batch) {
+                                left = 0;
+                                break;
+                            }
+                            r.load(p, b);
+                        } while (r.m == 0);
+                    }
+                }
+            }
+            if (x.hi > x.lo || x.nt == 0) return true;
+        }
+        return false;
+    }
+};
+
+// The CTA whose share has unit u: shares start at floor(c W / ctas).
+__device__ __forceinline__ int cta_of(long long u, long long W, int ctas) {
+    return (int)(((u + 1) * ctas - 1) / W);
+}
+
+// Every thread takes a run of requests; one of them finds where the CTA's share starts.
+__device__ void plan(const ChunkParams& p, Bars* s) {
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int per = (p.kv.batch + kThreads - 1) / kThreads;
+    const int b0 = min(p.kv.batch, tid * per), b1 = min(p.kv.batch, b0 + per);
+    Req r;
+    long long sum = 0;
+    for (int b = b0; b < b1; ++b) {
+        r.load(p, b);
+        sum += r.units(p) * p.kv.Hkv;
+    }
+    long long inc = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o *= 2) {
+        const long long y = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += y;
+    }
+    if (lane == 31) s->scan[warp] = inc;
+    if (tid == 0) s->left = 0;
+    __syncthreads();
+    long long before = 0, W = 0;
+    for (int k = 0; k < kThreads / 32; ++k) {
+        if (k < warp) before += s->scan[k];
+        W += s->scan[k];
+    }
+    before += inc - sum;
+    const int ctas = (int)max(1LL, min((long long)gridDim.x, W / p.min_units));
+    if (W == 0 || (int)blockIdx.x >= ctas) return;
+    const long long u0 = W * blockIdx.x / ctas, u1 = W * (blockIdx.x + 1) / ctas;
+    if (u0 < before || u0 >= before + sum) return;
+    long long at = before;
+    int b = b0;
+    for (; b < b1; ++b) {
+        r.load(p, b);
+        const long long c = r.units(p) * p.kv.Hkv;
+        if (u0 < at + c) break;
+        at += c;
+    }
+    const long long per_head = r.units(p);
+    const int g = (int)((u0 - at) / per_head);
+    at += g * per_head;
+    int lo = 0, hi = r.m - 1;  // the last item t with t + tiles_before(t) <= u0 - at
+    while (lo < hi) {
+        const int t = (lo + hi + 1) / 2;
+        if (t + r.tiles_before(p, t) <= u0 - at) lo = t;
+        else hi = t - 1;
+    }
+    at += lo + r.tiles_before(p, lo);
+    s->b = b;
+    s->g = g;
+    s->t = lo;
+    s->off = (int)(u0 - at);
+    s->U = at;
+    s->left = u1 - u0;
+    s->W = W;
+    s->ctas = ctas;
+}
+
+// ---- roles ----
+template <bool BF>
+__device__ void load_role(const ChunkParams& p, Bars* s, uint32_t smem) {
+    const int lane = threadIdx.x & 31;
+    const int P = 1 << p.kv.page_bits, box = min(P, kTile);
+    Walk w(p, s);
+    Piece x;
+    uint32_t fills = 0, pieces = 0, tails = 0;
+    bool ok = true;
+    while (ok && w.next(x)) {
+        if (x.nt == 0) continue;
+        const bool narrow = x.ntok <= p.tau;
+        // Q: row = token * G + head, as the box packs them
+        if (pieces && !warp_wait(s, &s->q_empty, (pieces - 1) & 1)) break;
+        ++pieces;
+        if (lane == 0) {
+            bar_expect(&s->q_full, (narrow ? 2 : 4) * 128 * p.G * p.tau);
+            for (int i = 0; i < (narrow ? 1 : 2); ++i)
+                for (int h = 0; h < 2; ++h)
+                    tma3(smem + i * kTileBytes + h * kHalf, &p.qmap, 64 * h, x.g * p.G,
+                         x.row0 + i * p.tau, &s->q_full);
+        }
+        const int32_t* row = p.kv.table + (int64_t)x.b * p.kv.table_stride;
+        // lane 2 i + h: half h of the i-th page (box) of a tile
+        auto page_of = [&](int j) {
+            const int tok = j * kTile + (lane >> 1) * box;
+            const int page = j < x.hi && (lane >> 1) * box < kTile && tok < x.len
+                                 ? row[tok >> p.kv.page_bits] : -1;
+            // an entry outside the cache: coordinates outside the map, which read as zeros
+            return page;
+        };
+        // (`done`: the stage's full barrier, or v_tail where something follows the copy)
+        auto fill = [&](const CUtensorMap* map, int j, int page, uint64_t* done) {
+            const int st = fills % kStages;
+            if (fills >= kStages && !warp_wait(s, &s->empty[st], (fills / kStages - 1) & 1))
+                return false;
+            ++fills;
+            if (!done) done = &s->full[st];
+            const int boxes = (min(kTile, x.len - j * kTile) + box - 1) / box;
+            if (lane == 0) bar_expect(done, boxes * box * 256);
+            __syncwarp();
+            const int i = lane >> 1, h = lane & 1;
+            if (i < boxes)
+                tma4(smem + (2 + st) * kTileBytes + h * kHalf + i * box * 128, map, 64 * h,
+                     (j * kTile + i * box) & (P - 1), x.g, page, done);
+            return true;
+        };
+        // wide items: K0 V0 K1 V1 ..; narrow ones: K0 K1, V0 K2, V1 K3, .. (the order of use)
+        int pk = page_of(x.lo), pk1 = page_of(x.lo + 1), pk2;
+        if (narrow) {
+            ok = fill(&p.kmap, x.lo, pk, nullptr);
+            if (ok && x.lo + 1 < x.hi) ok = fill(&p.kmap, x.lo + 1, pk1, nullptr);
+        }
+        for (int j = x.lo; ok && j < x.hi; ++j) {
+            pk2 = page_of(j + 2);
+            if (!narrow) ok = fill(&p.kmap, j, pk, nullptr);
+            if (!ok) break;
+            const int valid = x.len - j * kTile;
+            ok = fill(&p.vmap, j, pk, valid < kTile ? &s->v_tail : nullptr);
+            if (!ok) break;
+            if (valid < kTile) {  // the tile's rows past the last token: zeros
+                const int st = (fills - 1) % kStages;
+                if (!(ok = warp_wait(s, &s->v_tail, tails++ & 1))) break;
+                const uint32_t base = smem + (2 + st) * kTileBytes;
+                for (int i = valid * 8 + lane; i < kTile * 8; i += 32)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+                        asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};" ::"r"(
+                                         base + h * kHalf + i * 16),
+                                     "r"(0)
+                                     : "memory");
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) bar_arrive(&s->full[st]);
+            }
+            if (narrow && j + 2 < x.hi) ok = fill(&p.kmap, j + 2, pk2, nullptr);
+            pk = pk1;
+            pk1 = pk2;
+        }
+    }
+    // copies in flight end before the CTA does (only after a wait that ran out are there any)
+    if (*(volatile uint32_t*)&s->abort) {
+        for (uint32_t f = fills > kStages ? fills - kStages : 0; f < fills; ++f)
+            drain(&s->full[f % kStages], (f / kStages) & 1);
+        if (tails) drain(&s->v_tail, (tails - 1) & 1);
+        if (pieces) drain(&s->q_full, (pieces - 1) & 1);
+    }
+}
+
+template <bool BF>
+__device__ void mma_role(const ChunkParams& p, Bars* s, uint32_t smem, uint32_t tmem) {
+    constexpr uint32_t kFmt = BF ? 1u : 0u;
+    constexpr uint32_t kQk = 1u << 4 | kFmt << 7 | kFmt << 10 | (kTile / 8) << 17 | (kTile / 16) << 24;
+    constexpr uint32_t kPv = kQk | 1u << 16;  // B (V): N is the contiguous dimension
+    Walk w(p, s);
+    Piece x;
+    uint32_t use = 0, pieces = 0, np[2] = {0, 0};
+    auto stage = [&](uint32_t f) { return smem + (2 + f % kStages) * kTileBytes; };
+    auto wait_full = [&](uint32_t f) {
+        return bar_wait(s, &s->full[f % kStages], (f / kStages) & 1);
+    };
+    auto qk = [&](int i, int qt, uint32_t f) {
+        const uint32_t q = smem + qt * kTileBytes, k = stage(f);
+#pragma unroll
+        for (int kk = 0; kk < 8; ++kk) {
+            const uint32_t o = (kk >> 2) * kHalf + (kk & 3) * 32;
+            mma_ss(tmem + 128 * i, kdesc(q + o), kdesc(k + o), kQk, kk > 0);
+        }
+        commit(&s->s_full[i]);
+    };
+    auto pv = [&](int i, uint32_t f, bool first) {
+        const uint32_t v = stage(f);
+#pragma unroll
+        for (int kk = 0; kk < 8; ++kk)
+            mma_ts(tmem + 256 + 128 * i, tmem + 128 * i + 8 * kk, vdesc(v + kk * 2048), kPv,
+                   kk > 0 || !first);
+    };
+    auto wait_p = [&](int i) { return bar_wait(s, &s->p_full[i], np[i]++ & 1); };
+    bool ok = true;
+    while (ok && w.next(x)) {
+        if (x.nt == 0) continue;
+        const bool narrow = x.ntok <= p.tau;
+        if (!bar_wait(s, &s->q_full, pieces & 1)) break;
+        ++pieces;
+        const int n = x.hi - x.lo;
+        if (!narrow) {
+            uint32_t kf = use;  // fill of K_j; V_j is the next
+            if (!(ok = wait_full(kf))) break;
+            tc_after();
+            qk(0, 0, kf);
+            qk(1, 1, kf);
+            commit(&s->empty[kf % kStages]);
+            for (int j = 0; j < n; ++j, kf += 2) {
+                const bool more = j + 1 < n;
+                if (!more) commit(&s->q_empty);
+                if (!(ok = wait_full(kf + 1))) break;
+                if (more && !(ok = wait_full(kf + 2))) break;
+                for (int i = 0; i < 2; ++i) {
+                    if (!(ok = wait_p(i))) break;
+                    tc_after();
+                    pv(i, kf + 1, j == 0);
+                    if (more) qk(i, i, kf + 2);
+                    else commit(&s->o_full[i]);
+                }
+                if (!ok) break;
+                commit(&s->empty[(kf + 1) % kStages]);
+                if (more) commit(&s->empty[(kf + 2) % kStages]);
+            }
+            use += 2 * n;
+        } else {
+            // fills: K0 [K1] V0 [K2] V1 [K3] ..
+            uint32_t f = use;
+            for (int j = 0; j < min(n, 2); ++j, ++f) {
+                if (!(ok = wait_full(f))) break;
+                tc_after();
+                qk(j, 0, f);
+                commit(&s->empty[f % kStages]);
+            }
+            if (!ok) break;
+            if (n <= 2) commit(&s->q_empty);
+            for (int j = 0; j < n; ++j) {
+                const int i = j & 1;
+                if (!(ok = wait_full(f)) || !(ok = wait_p(i))) break;
+                tc_after();
+                pv(i, f, j < 2);
+                commit(&s->empty[f % kStages]);
+                ++f;
+                if (j + 2 < n) {
+                    if (!(ok = wait_full(f))) break;
+                    tc_after();
+                    qk(i, 0, f);
+                    commit(&s->empty[f % kStages]);
+                    ++f;
+                    if (j + 3 == n) commit(&s->q_empty);
+                } else {
+                    commit(&s->o_full[i]);
+                }
+            }
+            use = f;
+        }
+    }
+    if (*(volatile uint32_t*)&s->abort) {  // products in flight end before tensor memory is freed
+        commit(&s->drain);
+        drain(&s->drain, 0);
+    }
+}
+
+struct Pending {  // a split piece whose rows wait for the other parts
+    int on, slot, parts, index, first, row0, rows, g, narrow;
+};
+
+template <bool BF>
+__device__ void store_row(const ChunkParams& p, int64_t row, int head, const float (&o)[32], int c0,
+                          float f) {
+    uint16_t* dst = p.out + (row * p.Hq + head) * kPagedDim + c0;
+#pragma unroll
+    for (int c = 0; c < 32; c += 8) {
+        uint32_t u[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            u[e] = Half16<BF>::pack(o[c + 2 * e] * f, o[c + 2 * e + 1] * f);
+        *reinterpret_cast<uint4*>(dst + c) = make_uint4(u[0], u[1], u[2], u[3]);
+    }
+}
+
+// Add the parts of `rows` rows from r0: part k in slot (k == 0 ? 1 : 0) of CTA first + k, for narrow
+// items as two halves of rows.  A float4 of a row per thread.
+template <bool BF>
+__device__ void add_parts(const ChunkParams& p, const Pending& d, int r0, int r1) {
+    const int sources = d.narrow ? 2 * d.parts : d.parts;
+    auto base = [&](int k) {
+        const int part = d.narrow ? k >> 1 : k;
+        const int64_t slot = 2 * (int64_t)(d.first + part) + (part == 0 ? 1 : 0);
+        return slot * 2 * p.part_rows + (d.narrow && (k & 1) ? p.part_rows : 0);
+    };
+    auto row_in = [&](int r) {  // row r of the item: its place in a part
+        const int per = p.tau * p.G;
+        return d.narrow || r < per ? r : p.part_rows + r - per;
+    };
+    for (int e = threadIdx.x; e < (r1 - r0) * 32; e += 256) {
+        const int r = r0 + (e >> 5), c = e & 31, ri = row_in(r);
+        float M = -INFINITY;
+        for (int k = 0; k < sources; ++k) M = fmaxf(M, __ldcg(&p.ml[base(k) + ri]).x);
+        float l = 0.f;
+        float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int k = 0; k < sources; ++k) {
+            const float2 ml = __ldcg(&p.ml[base(k) + ri]);
+            if (ml.x == -INFINITY && ml.y == 0.f) continue;
+            const float f = ex2((ml.x - M) * p.scale_log2);
+            const float4 o =
+                __ldcg(reinterpret_cast<const float4*>(p.part + (base(k) + ri) * kPagedDim) + c);
+            l = fmaf(ml.y, f, l);
+            a.x = fmaf(o.x, f, a.x);
+            a.y = fmaf(o.y, f, a.y);
+            a.z = fmaf(o.z, f, a.z);
+            a.w = fmaf(o.w, f, a.w);
+        }
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        const int64_t row = d.row0 + r / p.G;
+        const int head = d.g * p.G + r % p.G;
+        *reinterpret_cast<uint2*>(p.out + (row * p.Hq + head) * kPagedDim + 4 * c) =
+            make_uint2(Half16<BF>::pack(a.x * inv, a.y * inv),
+                       Half16<BF>::pack(a.z * inv, a.w * inv));
+    }
+}
+
+template <bool BF>
+__device__ void softmax_role(const ChunkParams& p, Bars* s, uint32_t tmem) {
+    const int wg = threadIdx.x >> 7, r = threadIdx.x & 127, warp = threadIdx.x >> 5;
+    const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // the warp's 32 lanes of tensor memory
+    const uint32_t ts = tmem + lanes + 128 * wg, to = tmem + lanes + 256 + 128 * wg;
+    const float c = p.scale_log2, offset = BF ? 0.f : 7.f;
+    Walk w(p, s);
+    Piece x;
+    Pending pend[2] = {};
+    uint32_t ns = 0, no = 0, met = 0;
+    bool ok = true;
+    while (ok && w.next(x)) {
+        const bool narrow = x.ntok <= p.tau;
+        const int rows = x.ntok * p.G, per = p.tau * p.G;
+        const int r_item = narrow ? r : wg * per + r;  // row of the item
+        const bool valid = r < per && r_item < rows;
+        const int64_t orow = x.row0 + r_item / p.G;
+        const int ohead = x.g * p.G + r_item % p.G;
+        if (x.nt == 0) {  // no row of the item sees a token
+            if (valid && !(narrow && wg)) {
+                float z[32];
+#pragma unroll
+                for (int e = 0; e < 32; ++e) z[e] = 0.f;
+                for (int q = 0; q < 4; ++q) store_row<BF>(p, orow, ohead, z, 32 * q, 0.f);
+            }
+            continue;
+        }
+        const int seen = x.pos0 + (valid ? r_item / p.G : 0) + 1;     // tokens this row sees
+        const int least = x.pos0 + (narrow ? 0 : wg * p.tau) + 1;    // .. the tile's first row sees
+        float m = -INFINITY, l = 0.f;
+        bool first = true;
+        for (int j = x.lo + (narrow ? wg : 0); j < x.hi; j += narrow ? 2 : 1) {
+            if (!(ok = warp_wait(s, &s->s_full[wg], ns++ & 1))) break;
+            tc_after();
+            float v[128];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) tm_ld32(ts + 32 * q, v + 32 * q);
+            tm_wait_ld();
+#pragma unroll
+            for (int q = 0; q < 4; ++q) pin32(v + 32 * q);
+            if ((j + 1) * kTile > least) {
+                const int lim = seen - j * kTile;
+#pragma unroll
+                for (int e = 0; e < 128; ++e)
+                    if (e >= lim) v[e] = -INFINITY;
+            }
+            float mx[4] = {v[0], v[1], v[2], v[3]};
+#pragma unroll
+            for (int e = 4; e < 128; ++e) mx[e & 3] = fmaxf(mx[e & 3], v[e]);
+            const float mn = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+            if (first) {
+                m = mn;
+                first = false;
+            } else {
+                // (the product that last changed O is complete: S came after it)
+                const bool grow = valid && (mn - m) * c > kGrow;
+                if (__any_sync(0xffffffffu, grow)) {
+                    const float to_m = fmaxf(m, mn);
+                    const float f = to_m == -INFINITY ? 1.f : ex2((m - to_m) * c);
+                    m = to_m;
+                    l *= f;
+                    for (int q = 0; q < 4; ++q) {
+                        float o[32];
+                        tm_ld32(to + 32 * q, o);
+                        tm_wait_ld();
+                        pin32(o);
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) o[e] *= f;
+                        tm_st32(to + 32 * q, reinterpret_cast<const uint32_t*>(o));
+                    }
+                }
+            }
+            const float base = (m == -INFINITY ? 0.f : m * c) - offset;
+            float sum[4] = {0.f, 0.f, 0.f, 0.f};
+            uint32_t pk[64];
+#pragma unroll
+            for (int e = 0; e < 128; e += 2) {
+                const float a = ex2(fmaf(v[e], c, -base)), b = ex2(fmaf(v[e + 1], c, -base));
+                sum[(e >> 1) & 3] += a + b;
+                pk[e >> 1] = Half16<BF>::pack(a, b);
+            }
+            tm_st32(ts, pk);
+            tm_st32(ts + 32, pk + 32);
+            tm_wait_st();
+            tc_before();
+            __syncwarp();
+            if ((threadIdx.x & 31) == 0) bar_arrive(&s->p_full[wg]);
+            l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        }
+        if (!ok) break;
+        const bool direct = !narrow && x.whole();
+        const int slot = x.lo > 0 ? 0 : 1;
+        const int64_t part = (2 * (int64_t)blockIdx.x + slot) * 2 * p.part_rows + wg * p.part_rows + r;
+        if (!first) {
+            if (!(ok = warp_wait(s, &s->o_full[wg], no++ & 1))) break;
+            tc_after();
+            const float inv = l == 0.f ? 0.f : 1.f / l;
+            for (int q = 0; q < 4; ++q) {
+                float o[32];
+                tm_ld32(to + 32 * q, o);
+                tm_wait_ld();
+                pin32(o);
+                if (valid && direct) {
+                    store_row<BF>(p, orow, ohead, o, 32 * q, inv);
+                } else if (valid) {
+                    float4* dst = reinterpret_cast<float4*>(p.part + part * kPagedDim + 32 * q);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        __stcg(dst + e, make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2],
+                                                    o[4 * e + 3]));
+                }
+                __syncwarp();
+            }
+            tc_before();  // (the next item's first product comes after the next P)
+        }
+        if (direct) continue;
+        if (valid) __stcg(&p.ml[part], make_float2(m, l));
+        Pending d;
+        const int cf = cta_of(x.U + 1, s->W, s->ctas), cl = cta_of(x.U + x.nt, s->W, s->ctas);
+        d = Pending{1, slot, cl - cf + 1, (int)blockIdx.x - cf, cf, x.row0, rows, x.g, narrow};
+        if (d.parts == 1) {  // a narrow item of this CTA alone
+            if (!(ok = meet(s, met))) break;
+            add_parts<BF>(p, d, 0, rows);
+            if (!(ok = meet(s, met))) break;
+        } else {
+            __threadfence();
+            if (!(ok = meet(s, met))) break;
+            if (threadIdx.x == 0) atomicAdd(&p.count[cf], 1u);
+            pend[slot] = d;
+        }
+    }
+    // the split pieces, once all their parts are there
+    for (int k = 0; ok && k < 2; ++k) {
+        const Pending d = pend[k];
+        if (!d.on) continue;
+        if (threadIdx.x == 0) {
+            uint32_t n = 0;
+            const long long t0 = clock64();
+            do {
+                asm volatile("ld.acquire.gpu.global.u32 %0, [%1];"
+                             : "=r"(n)
+                             : "l"(p.count + d.first)
+                             : "memory");
+                if (n >= (uint32_t)d.parts) break;
+                __nanosleep(32);
+            } while (clock64() - t0 < kWaitCycles);
+            if (n < (uint32_t)d.parts) *(volatile uint32_t*)&s->abort = 1;
+        }
+        if (!(ok = meet(s, met)) || *(volatile uint32_t*)&s->abort) break;
+        __threadfence();
+        add_parts<BF>(p, d, (int)((long long)d.rows * d.index / d.parts),
+                      (int)((long long)d.rows * (d.index + 1) / d.parts));
+        if (threadIdx.x == 0) {  // the last to have seen the count clears it
+            if (atomicAdd(&p.done[d.first], 1u) == (uint32_t)d.parts - 1) {
+                p.count[d.first] = 0;
+                p.done[d.first] = 0;
+            }
+        }
+    }
+}
+
+template <bool BF>
+__global__ void __launch_bounds__(kThreads, 1) paged_chunk_kernel(
+    const __grid_constant__ ChunkParams p) {
+    extern __shared__ uint8_t raw[];
+    const uint32_t smem = (s32(raw) + 1023u) & ~1023u;
+    Bars* s = reinterpret_cast<Bars*>(raw + (smem - s32(raw)) + kSmemTiles);
+    const int warp = threadIdx.x >> 5;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kStages; ++i) {
+            bar_init(&s->full[i], 1);
+            bar_init(&s->empty[i], 1);
+        }
+        bar_init(&s->q_full, 1);
+        bar_init(&s->q_empty, 1);
+        bar_init(&s->v_tail, 1);
+        bar_init(&s->drain, 1);
+        bar_init(&s->soft, 8);
+        for (int i = 0; i < 2; ++i) {
+            bar_init(&s->s_full[i], 1);
+            bar_init(&s->p_full[i], 4);
+            bar_init(&s->o_full[i], 1);
+        }
+        s->abort = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 9) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(
+                         s32(&s->tmem))
+                     : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    plan(p, s);
+    tc_before();
+    __syncthreads();
+    tc_after();
+    const uint32_t tmem = s->tmem;
+    if (warp < 8) {
+        softmax_role<BF>(p, s, tmem);
+    } else if (warp == 8) {
+        load_role<BF>(p, s, smem);
+    } else if ((threadIdx.x & 31) == 0) {
+        mma_role<BF>(p, s, smem, tmem);
+    }
+    __syncwarp();
+    tc_before();
+    __syncthreads();
+    tc_after();
+    if (warp == 9)
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem)
+                     : "memory");
+    if (threadIdx.x == 0 && s->abort) atomicExch(p.status, (uint32_t)LAQ_ERR_TIMEOUT);
+}
+
+typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*,
+                                const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                                const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiled encode_tiled() {
+    static std::atomic<EncodeTiled> fn{nullptr};
+    EncodeTiled f = fn.load();
+    if (!f) {
+        void* e = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &e, 12000, cudaEnableDefault,
+                                             &q) != cudaSuccess ||
+            q != cudaDriverEntryPointSuccess)
+            return nullptr;
+        f = reinterpret_cast<EncodeTiled>(e);
+        fn.store(f);
+    }
+    return f;
+}
+
+bool encode(CUtensorMap* m, bool bf, int rank, const void* base, const cuuint64_t* dims,
+            const cuuint64_t* strides, const cuuint32_t* box) {
+    const EncodeTiled f = encode_tiled();
+    const cuuint32_t one[4] = {1, 1, 1, 1};
+    return f && f(m, bf ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16,
+                  (cuuint32_t)rank, const_cast<void*>(base), dims, strides, box, one,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                  CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+constexpr int kMaxCtas = 256;
+constexpr size_t kHeader = 4096;  // status, counters
+
+int part_rows(int64_t max_q, int G) {
+    const int64_t per = 128 / G * G, rows = max_q * G;
+    return (int)(rows < per ? rows : per);
+}
+
+}  // namespace
+
+size_t chunk_workspace_bytes(int64_t max_q, int G) {
+    const size_t rows = (size_t)kMaxCtas * 4 * part_rows(max_q, G);
+    return kHeader + rows * (kPagedDim * sizeof(float) + sizeof(float2));
+}
+
+laq_status launch_chunk(const PagedKv& kv, bool bf, const void* q, int64_t q_stride, int T, int max_q,
+                        int Hq, float scale, void* out, void* workspace, cudaStream_t stream) {
+    static std::atomic<int> sms_of[kMaxDevices];
+    const void* fn = bf ? (const void*)paged_chunk_kernel<true> : (const void*)paged_chunk_kernel<false>;
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return LAQ_ERR_CUDA;
+    int sms = sms_of[dev].load();
+    if (sms == 0) {
+        if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess ||
+            cudaFuncSetAttribute((const void*)paged_chunk_kernel<true>,
+                                 cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem) != cudaSuccess ||
+            cudaFuncSetAttribute((const void*)paged_chunk_kernel<false>,
+                                 cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem) != cudaSuccess)
+            return LAQ_ERR_CUDA;
+        if (sms > kMaxCtas) sms = kMaxCtas;
+        sms_of[dev].store(sms);
+    }
+    ChunkParams p = {};
+    p.kv = kv;
+    p.G = Hq / kv.Hkv;
+    p.Hq = Hq;
+    p.tau = 128 / p.G;
+    p.T = T;
+    p.max_q = max_q;
+    p.min_units = 4;
+    p.part_rows = part_rows(max_q, p.G);
+    p.scale_log2 = scale * 1.44269504088896340736f;
+    p.out = static_cast<uint16_t*>(out);
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
+    p.status = reinterpret_cast<uint32_t*>(ws);
+    p.count = p.status + 64;
+    p.done = p.count + kMaxCtas;
+    const size_t rows = (size_t)kMaxCtas * 4 * p.part_rows;
+    p.part = reinterpret_cast<float*>(ws + kHeader);
+    p.ml = reinterpret_cast<float2*>(p.part + rows * kPagedDim);
+    const int P = 1 << kv.page_bits, box = P < kTile ? P : kTile;
+    const cuuint64_t kd[4] = {kPagedDim, (cuuint64_t)P, (cuuint64_t)kv.Hkv, (cuuint64_t)kv.pages};
+    const cuuint64_t ks[3] = {(cuuint64_t)kv.token_stride * 2, (cuuint64_t)kv.head_stride * 2,
+                              (cuuint64_t)kv.page_stride * 2};
+    const cuuint32_t kb[4] = {64, (cuuint32_t)box, 1, 1};
+    const cuuint64_t qd[3] = {kPagedDim, (cuuint64_t)Hq, (cuuint64_t)T};
+    const cuuint64_t qs[2] = {kPagedDim * 2, (cuuint64_t)q_stride * 2};
+    const cuuint32_t qb[3] = {64, (cuuint32_t)p.G, (cuuint32_t)p.tau};
+    if (!encode(&p.kmap, bf, 4, kv.k, kd, ks, kb) || !encode(&p.vmap, bf, 4, kv.v, kd, ks, kb) ||
+        !encode(&p.qmap, bf, 3, q, qd, qs, qb))
+        return LAQ_ERR_CUDA;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)sms);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = kSmem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeCooperative;
+    attr[0].val.cooperative = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    void* args[] = {&p};
+    return cudaLaunchKernelExC(&cfg, fn, args) == cudaSuccess ? LAQ_OK : LAQ_ERR_CUDA;
+}
+
+}  // namespace laq

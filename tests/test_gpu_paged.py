@@ -105,7 +105,7 @@ def test_attention(n, L, P, Hq, Hkv, dtype, order):
                 c[int(table[b, x // P]), :, x % P:] = float("nan")
     cache = _lib.PagedCache(k, v, torch.from_numpy(table).cuda(), torch.from_numpy(q_start).cuda(),
                             torch.tensor(L, dtype=torch.int32).cuda())
-    ws = _lib.paged_attention_workspace(sum(n), len(n), max(n), Hq, Hkv, "cuda")
+    ws = _lib.paged_attention_workspace(sum(n), len(n), max(n) + 100, Hq, Hkv, "cuda")
     out = torch.full((sum(n), Hq, D), float("nan"), dtype=dtype, device="cuda")
     for _ in range(2):   # the workspace serves again
         _lib.laq_paged_attention(q, cache, max(n), SCALE, ws, out=out)
