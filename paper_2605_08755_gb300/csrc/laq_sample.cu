@@ -1,51 +1,47 @@
 // laq_sample.cu -- the next token of each row of logits: temperature, top-k, top-p and min-p, and the
 // choice by a given random number.
 //
-// Weights are whole numbers (2^40 for the maximum), so that every sum is exact and no result depends
-// on how a sum is split; logits map to 32-bit keys of the same order.  What top-k and top-p keep is a
-// prefix of the order (key descending, index ascending): all keys above some key, and the first few
-// of that key.  The prefix is found digit by digit of the key (a histogram of counts and weights per
-// digit), the token by prefix sums of the kept weights in the order of the index.
+// Weights are whole numbers (2^40 for the maximum), so that every sum is exact, integer atomics give
+// one result in any order, and no result depends on how a row is split.  What top-k and top-p keep is
+// a prefix of the order (logit descending, index ascending), found in three steps:
+//   1. a histogram of the row in 2048 bins of equal width below its maximum (of counts for top-k; of
+//      weights and counts for top-p), whose prefix sums name the bin that the cut falls in;
+//   2. the elements of that bin, or, where the whole prefix up to it is small (the usual case), all
+//      elements up to it, are gathered into a list and sorted;
+//   3. prefix sums over the sorted list give the cut to the element.
+// A list that would not fit is refined by further histograms of the elements' keys (order-preserving
+// bits of the logit, then of the index).  With the whole prefix in the list the token is chosen there;
+// otherwise a last pass sums the kept weights in the order of the index.
+//
+// A cluster of C CTAs works on a row, each on a slice that it reads once and keeps in shared memory
+// (a slice that does not fit is read again, from L2).  Histograms meet by distributed shared memory,
+// the list lies in CTA 0.
+// The quotient (x - top) / t costs a compiler's division ten instructions for each logit; a row's t is
+// one number, so it is formed from the rounded reciprocal with one correction (Markstein, IBM J. Res.
+// Dev. 34, 1990), which gives the correctly rounded quotient.
+#include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "laq.h"
 #include "laq_device.cuh"
+#include "laq_internal.cuh"
+
+namespace cg = cooperative_groups;
 
 namespace laq {
 namespace {
 
-constexpr int kThreads = 1024;
 typedef unsigned long long u64;
-
-template <int DT>
-__device__ __forceinline__ float load_logit(const void* row, int64_t i) {
-    float x;
-    if (DT == LAQ_F32) x = static_cast<const float*>(row)[i];
-    else if (DT == LAQ_F16) x = __half2float(static_cast<const __half*>(row)[i]);
-    else x = __bfloat162float(static_cast<const __nv_bfloat16*>(row)[i]);
-    return isnan(x) ? -INFINITY : x + 0.f;  // (+ 0: the two zeros are one value)
-}
-// order-preserving key
-__device__ __forceinline__ uint32_t key_of(float x) {
-    const uint32_t b = __float_as_uint(x);
-    return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
-}
-__device__ __forceinline__ u64 weight(float x, float top, float t) {
-    return x == top ? (u64)1 << 40 : (u64)(expf((x - top) / t) * 0x1p40f);
-}
-// floor(mass * f / 2^24), mass < 2^63, f <= 2^24
-__device__ __forceinline__ u64 part(u64 mass, uint32_t f) {
-    return (mass >> 24) * f + (((mass & 0xffffffu) * f) >> 24);
-}
-
-// What is kept: keys above `key`, and the first `count` (by index) of those equal to it.
-struct Cut {
-    uint32_t key;
-    u64 count;
-};
+constexpr int kBins = 2048;
+constexpr int kList = 2048;        // elements of the list
+constexpr int kIdxBits = 22;       // V <= 2^22
+constexpr int kMaxWarps = 32;
+constexpr int kMaxC = 8;
 
 struct SampleParams {
     const void* logits;
@@ -54,185 +50,583 @@ struct SampleParams {
     int32_t* out;
     float* p_out;
     int64_t row_stride;
-    int V;
+    int V, C, slice, resident;  // slice: elements per CTA (a multiple of 8); resident: kept in smem
 };
 
-template <typename T>
-__device__ __forceinline__ T block_sum(T v, T* red) {
+struct SampleSmem {
+    uint32_t cnt[kBins], lo[kBins], hi[kBins];
+    u64 list[kList];
+    u64 red[kMaxWarps], red2[kMaxWarps];
+    float fred[2][kMaxWarps];
+    float2 ends[kMaxC];          // (max, min) of every CTA of the cluster
+    u64 sums[kMaxC];             // kept weight of every CTA
+    u64 found[4], cut;
+    uint32_t n_list, first;
+};
+
+template <int DT>
+struct Logits;  // 16 bytes of logits as floats; NaN as -inf, -0 as 0
+template <>
+struct Logits<LAQ_F32> {
+    static constexpr int kPer = 4, kSize = 4;
+    static __device__ __forceinline__ void unpack(const uint4& u, float (&x)[kPer]) {
+        x[0] = __uint_as_float(u.x); x[1] = __uint_as_float(u.y);
+        x[2] = __uint_as_float(u.z); x[3] = __uint_as_float(u.w);
+    }
+    static __device__ __forceinline__ uint32_t raw(const void* p, int64_t i) {
+        return static_cast<const uint32_t*>(p)[i];
+    }
+};
+template <bool BF>
+struct Logits16 {
+    static constexpr int kPer = 8, kSize = 2;
+    static __device__ __forceinline__ void unpack(const uint4& u, float (&x)[kPer]) {
+        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+        for (int i = 0; i < 4; ++i) {
+            if (BF) {
+                x[2 * i] = __uint_as_float(w[i] << 16);
+                x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+            } else {
+                const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+                x[2 * i] = f.x;
+                x[2 * i + 1] = f.y;
+            }
+        }
+    }
+    static __device__ __forceinline__ uint32_t raw(const void* p, int64_t i) {
+        return static_cast<const uint16_t*>(p)[i];
+    }
+};
+template <>
+struct Logits<LAQ_F16> : Logits16<false> {};
+template <>
+struct Logits<LAQ_BF16> : Logits16<true> {};
+
+__device__ __forceinline__ float clean(float x) { return isnan(x) ? -INFINITY : x + 0.f; }
+
+// order-preserving key of a logit, and back
+__device__ __forceinline__ uint32_t key_of(float x) {
+    const uint32_t b = __float_as_uint(x);
+    return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float logit_of(uint32_t key) {
+    return __uint_as_float((key & 0x80000000u) ? key ^ 0x80000000u : ~key);
+}
+// place in the order: larger first
+__device__ __forceinline__ u64 place(float x, int idx) {
+    return (u64)key_of(x) << kIdxBits | (u64)((1 << kIdxBits) - 1 - idx);
+}
+__device__ __forceinline__ float place_logit(u64 c) { return logit_of((uint32_t)(c >> kIdxBits)); }
+__device__ __forceinline__ int place_index(u64 c) {
+    return (1 << kIdxBits) - 1 - (int)(c & ((1u << kIdxBits) - 1));
+}
+// floor(mass * f / 2^24), mass < 2^63, f <= 2^24
+__device__ __forceinline__ u64 part(u64 mass, uint32_t f) {
+    return (mass >> 24) * f + (((mass & 0xffffffu) * f) >> 24);
+}
+
+// A row's weights.
+struct Weights {
+    float top, t, r;
+    bool plain;  // t so large or small that its reciprocal is not a normal number
+    __device__ Weights(float top_, float t_) : top(top_), t(t_), r(1.f / t_) {
+        plain = !(t > 0x1p-100f && t < 0x1p100f);
+    }
+    __device__ __forceinline__ u64 operator()(float x) const {
+        const float d = x - top;
+        float q;
+        if (plain) {
+            q = x == -INFINITY ? -INFINITY : d / t;
+        } else {
+            q = fmaxf(d * r, -64.f);  // (past -28 the weight is 0: the bound keeps -inf apart from +inf)
+            q = fmaf(fmaf(-q, t, d), r, q);
+        }
+        const u64 w = (u64)(expf(q) * 0x1p40f);
+        return x == top ? (u64)1 << 40 : w;
+    }
+};
+
+template <int DT>
+struct Row {
+    static constexpr int kPer = Logits<DT>::kPer;
+    const uint8_t* src;   // the slice: shared memory (16-byte aligned) or global
+    int n, i0;            // its elements, the first one's index in the row
+    bool aligned;
+
+    __device__ __forceinline__ uint4 raw(int c) const {
+        if (aligned) {
+            if (kPer * (c + 1) <= n) return *reinterpret_cast<const uint4*>(src + 16 * (size_t)c);
+        }
+        uint32_t e[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+        for (int k = 0; k < kPer; ++k) {
+            const int i = kPer * c + k;
+            const uint32_t v = i < n ? Logits<DT>::raw(src, i) : 0u;
+            if (kPer == 4) e[k] = v;
+            else e[k >> 1] |= v << (16 * (k & 1));
+        }
+        return make_uint4(e[0], e[1], e[2], e[3]);
+    }
+    // f(x, index in the row) of the calling thread's elements, chunks of 16 bytes strided over the CTA
+    template <typename F>
+    __device__ __forceinline__ void each(F f) const {
+        const int chunks = (n + kPer - 1) / kPer;
+        for (int c = threadIdx.x; c < chunks; c += blockDim.x) {
+            float x[kPer];
+            Logits<DT>::unpack(raw(c), x);
+            const int m = n - kPer * c;
+#pragma unroll
+            for (int k = 0; k < kPer; ++k)
+                if (k < m) f(clean(x[k]), i0 + kPer * c + k);
+        }
+    }
+};
+
+__device__ __forceinline__ u64 warp_scan(u64 v) {  // inclusive
+#pragma unroll
+    for (int o = 1; o < 32; o *= 2) {
+        const u64 y = __shfl_up_sync(0xffffffffu, v, o);
+        if ((threadIdx.x & 31) >= o) v += y;
+    }
+    return v;
+}
+// exclusive prefix over the CTA and the total (two barriers)
+__device__ __forceinline__ u64 block_scan(u64 v, u64* red, u64* total) {
+    const int warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+    const u64 inc = warp_scan(v);
     __syncthreads();
-    if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = v;
+    if ((threadIdx.x & 31) == 31) red[warp] = inc;
     __syncthreads();
-    T s = 0;
-    for (int k = 0; k < kThreads / 32; ++k) s += red[k];
-    return s;
+    const u64 w = (threadIdx.x & 31) < warps ? red[threadIdx.x & 31] : 0;
+    const u64 s = warp_scan(w);
+    *total = __shfl_sync(0xffffffffu, s, 31);
+    const u64 before = __shfl_sync(0xffffffffu, s - w, warp);
+    return before + inc - v;
+}
+
+// Sort the first n of list, padded to a power of two with `pad`; descending or ascending.
+__device__ __forceinline__ void sort_list(u64* list, int n, bool descending) {
+    int N = 32;
+    while (N < n) N *= 2;
+    for (int i = n + threadIdx.x; i < N; i += blockDim.x) list[i] = descending ? 0 : ~(u64)0;
+    for (int k = 2; k <= N; k *= 2)
+        for (int j = k / 2; j > 0; j /= 2) {
+            __syncthreads();
+            for (int i = threadIdx.x; i < N / 2; i += blockDim.x) {
+                const int a = (i / j) * 2 * j + i % j, b = a + j;
+                const u64 x = list[a], y = list[b];
+                const bool up = ((a & k) == 0) != descending;  // this run ascends
+                if ((x > y) == up) {
+                    list[a] = y;
+                    list[b] = x;
+                }
+            }
+        }
+    __syncthreads();
 }
 
 template <int DT>
-__global__ void __launch_bounds__(kThreads) sample_kernel(const SampleParams p) {
+__global__ void __launch_bounds__(1024) sample_kernel(const SampleParams p) {
+    extern __shared__ __align__(16) uint8_t dyn[];
+    SampleSmem& s = *reinterpret_cast<SampleSmem*>(dyn);
+    uint8_t* slice = dyn + sizeof(SampleSmem);
+    static_assert(sizeof(SampleSmem) % 16 == 0, "the slice is 16-byte aligned");
     pdl_launch_dependents();
+    cg::cluster_group cluster = cg::this_cluster();
+    const int C = p.C, rank = C > 1 ? (int)cluster.block_rank() : 0;
+    const int tid = threadIdx.x, nt = blockDim.x, warp = tid >> 5, lane = tid & 31;
+    const int m = blockIdx.x / C, V = p.V;
+    auto all_sync = [&] {
+        if (C > 1) cluster.sync();
+        else __syncthreads();
+    };
+    auto remote = [&](auto* ptr, int r) { return C > 1 ? cluster.map_shared_rank(ptr, r) : ptr; };
     pdl_wait();
-    __shared__ u64 red[32], hist_w[256];
-    __shared__ uint32_t hist_n[256];
-    __shared__ u64 pick[4];
-    __shared__ float fred[32];
-    const int m = blockIdx.x, V = p.V, tid = threadIdx.x;
-    const size_t size = DT == LAQ_F32 ? 4 : 2;
-    const void* row = static_cast<const char*>(p.logits) + (size_t)m * p.row_stride * size;
-    float top = -INFINITY;
-    for (int i = tid; i < V; i += kThreads) top = fmaxf(top, load_logit<DT>(row, i));
+    Row<DT> row;
+    row.i0 = min(V, rank * p.slice);
+    row.n = min(V - row.i0, p.slice);
+    row.src = static_cast<const uint8_t*>(p.logits) +
+              ((size_t)m * p.row_stride + row.i0) * Logits<DT>::kSize;
+    row.aligned = ((uintptr_t)row.src & 15u) == 0;
+
+    // ---- one pass over the row: the slice into shared memory, its largest and least element ----
+    float top = -INFINITY, bot = INFINITY;
+    {
+        constexpr int kPer = Row<DT>::kPer, kDeep = 4;
+        const int chunks = (row.n + kPer - 1) / kPer;
+        for (int c0 = tid; c0 < chunks; c0 += kDeep * nt) {
+            uint4 u[kDeep];
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-    if ((tid & 31) == 0) fred[tid >> 5] = top;
+            for (int a = 0; a < kDeep; ++a)
+                if (c0 + a * nt < chunks) u[a] = row.raw(c0 + a * nt);
+#pragma unroll
+            for (int a = 0; a < kDeep; ++a) {
+                const int c = c0 + a * nt;
+                if (c >= chunks) break;
+                if (p.resident) *reinterpret_cast<uint4*>(slice + 16 * (size_t)c) = u[a];
+                float x[kPer];
+                Logits<DT>::unpack(u[a], x);
+#pragma unroll
+                for (int k = 0; k < kPer; ++k)
+                    if (kPer * c + k < row.n) {
+                        const float y = clean(x[k]);
+                        top = fmaxf(top, y);
+                        if (y > -INFINITY) bot = fminf(bot, y);
+                    }
+            }
+        }
+        if (p.resident) {
+            row.src = slice;
+            row.aligned = true;
+        }
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        bot = fminf(bot, __shfl_xor_sync(0xffffffffu, bot, o));
+    }
+    if (lane == 0) {
+        s.fred[0][warp] = top;
+        s.fred[1][warp] = bot;
+    }
+    if (tid == 0) {
+        s.n_list = 0;
+        s.first = 0xffffffffu;
+    }
+    auto clear_bins = [&] {
+        for (int i = tid; i < kBins; i += nt) s.cnt[i] = s.lo[i] = s.hi[i] = 0;
+    };
+    clear_bins();
     __syncthreads();
-    for (int k = 0; k < 32; ++k) top = fmaxf(top, fred[k]);
-    if (top == -INFINITY) {
-        if (tid == 0) {
+    if (warp == 0) {
+        top = lane < nt / 32 ? s.fred[0][lane] : -INFINITY;
+        bot = lane < nt / 32 ? s.fred[1][lane] : INFINITY;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+            bot = fminf(bot, __shfl_xor_sync(0xffffffffu, bot, o));
+        }
+    }
+    // (every CTA of the cluster has to have started before its shared memory is written)
+    if (C > 1) cluster.sync();
+    if (warp == 0 && lane < C) remote(&s.ends[0], lane)[rank] = make_float2(top, bot);
+    all_sync();
+    top = -INFINITY, bot = INFINITY;
+    for (int r = 0; r < C; ++r) {
+        top = fmaxf(top, s.ends[r].x);
+        bot = fminf(bot, s.ends[r].y);
+    }
+    if (top == -INFINITY) {  // (all CTAs of the cluster agree)
+        if (rank == 0 && tid == 0) {
             p.out[m] = 0;
             if (p.p_out) p.p_out[m] = 0.f;
         }
         return;
     }
-    float t = p.temperature ? p.temperature[m] : 1.f;
-    const bool greedy = !(t > 0.f);
+
+    // ---- the row's settings ----
+    const float t_in = p.temperature ? p.temperature[m] : 1.f;
     int64_t k = p.top_k ? p.top_k[m] : 0;
     if (k <= 0 || k > V) k = V;
-    if (greedy) {
-        k = 1;
-        t = 1.f;
+    if (!(t_in > 0.f) || (k == 1 && V > 1) || V == 1) {  // the first maximum
+        uint32_t first = 0xffffffffu;
+        row.each([&](float x, int i) {
+            if (x == top) first = min(first, (uint32_t)i);
+        });
+        first = __reduce_min_sync(0xffffffffu, first);
+        if (lane == 0 && first != 0xffffffffu) atomicMin(remote(&s.first, 0), first);
+        all_sync();
+        if (rank == 0 && tid == 0) {
+            p.out[m] = (int32_t)s.first;
+            if (p.p_out) p.p_out[m] = 1.f;
+        }
+        return;
     }
+    const Weights weight(top, t_in);
     const float fp = p.top_p ? p.top_p[m] : 1.f, fm = p.min_p ? p.min_p[m] : 0.f;
-    const bool use_p = fp < 1.f && !greedy;
+    const bool use_p = fp < 1.f;
     const uint32_t pf = use_p ? (uint32_t)(fmaxf(fp, 0.f) * 0x1p24f) : 0u;
-    const u64 floor_w = fm > 0.f && !greedy ? (u64)(fminf(fm, 1.f) * 0x1p40f) : 0;
+    const u64 floor_w = fm > 0.f ? (u64)(fminf(fm, 1.f) * 0x1p40f) : 0;
     const float u = p.u[m];
     const uint32_t uf = u > 0.f ? min((uint32_t)(fminf(u, 1.f) * 0x1p24f), 0xffffffu) : 0u;
 
-    // The shortest prefix of the order, within `in`, of `need` elements or (BY_MASS) of a weight of at
-    // least `need`; *mass: the prefix's weight.
-    auto find = [&](bool by_mass, u64 need, u64* mass) {
-        uint32_t prefix = 0;
-        u64 above_w = 0;
-        Cut cut = {0u, 0};
-        for (int shift = 24; shift >= 0; shift -= 8) {
-            if (tid < 256) hist_n[tid] = 0, hist_w[tid] = 0;
-            __syncthreads();
-            for (int i = tid; i < V; i += kThreads) {
-                const float x = load_logit<DT>(row, i);
-                const uint32_t key = key_of(x);
-                if (shift < 24 && (key >> (shift + 8)) != (prefix >> (shift + 8))) continue;
-                atomicAdd(&hist_n[(key >> shift) & 255], 1u);
-                atomicAdd(&hist_w[(key >> shift) & 255], weight(x, top, t));
-            }
-            __syncthreads();
-            if (tid == 0) {
-                int d = 255;
-                u64 w = above_w, left = need;
-                for (; d > 0; --d) {
-                    const u64 a = by_mass ? hist_w[d] : hist_n[d];
-                    if (a >= left && hist_n[d]) break;
-                    left -= min(a, left);
-                    w += hist_w[d];
-                }
-                pick[0] = d;
-                pick[1] = left;
-                pick[2] = w;
-                pick[3] = hist_n[d];
-            }
-            __syncthreads();
-            prefix |= (uint32_t)pick[0] << shift;
-            need = pick[1];
-            above_w = pick[2];
-            cut.count = pick[3];
-            __syncthreads();
-        }
-        cut.key = prefix;
-        // elements of the last key: all of one weight
-        const uint32_t b = (prefix & 0x80000000u) ? prefix ^ 0x80000000u : ~prefix;
-        const u64 w = weight(__uint_as_float(b), top, t);
-        if (by_mass) cut.count = w ? min(cut.count, max((u64)1, (need + w - 1) / w)) : cut.count;
-        else cut.count = need;
-        *mass = above_w + cut.count * w;
-        return cut;
+    u64 cut = 0;        // what is kept: elements whose place is at least this
+    float scale = 0.f;  // bins per unit of logit
+    auto bin_of = [&](float x) {
+        return x == top ? 0 : (int)fminf((top - x) * scale, (float)(kBins - 1));
     };
-    u64 mass = 0;
-    Cut cut = {0u, 0x7fffffff};
-    bool cut_on = false;
-    if (k < V) {
-        cut = find(false, (u64)k, &mass);
-        cut_on = true;
-    }
-    if (use_p) {
-        if (!cut_on) {
-            u64 s = 0;
-            for (int i = tid; i < V; i += kThreads) s += weight(load_logit<DT>(row, i), top, t);
-            mass = block_sum(s, red);
+    auto add_mass = [&](int b, u64 w) {  // 64 bits in two words: the low one's wrap is a carry
+        const uint32_t wl = (uint32_t)w, old = atomicAdd(&s.lo[b], wl);
+        const uint32_t up = (uint32_t)(w >> 32) + (old + wl < old);
+        if (up) atomicAdd(&s.hi[b], up);
+    };
+    // The cluster's bins: prefix sums of counts or weights; the bin where they reach `need` (all
+    // threads of all CTAs get the same).  found: bin, what is left of `need` in it, the elements of the
+    // bin, the elements up to and with it.  Returns the sum over all bins.  *need may depend on that sum.
+    auto find_bin = [&](bool by_mass, auto need_of) {
+        all_sync();
+        const int per = kBins / nt > 0 ? kBins / nt : 1;  // nt divides kBins
+        u64 v[8], n[8], sv = 0, sn = 0;
+        for (int i = 0; i < per; ++i) {
+            const int b = tid * per + i;
+            u64 w = 0, c = 0;
+            for (int r = 0; r < C; ++r) {
+                c += remote(s.cnt, r)[b];
+                if (by_mass)
+                    w += (u64)remote(s.lo, r)[b] + ((u64)remote(s.hi, r)[b] << 32);
+            }
+            n[i] = c;
+            v[i] = by_mass ? w : c;
+            sv += v[i];
+            sn += c;
         }
-        cut = find(true, max((u64)1, part(mass, pf)), &mass);
-        cut_on = true;
+        u64 total, all;
+        u64 at = block_scan(sv, s.red, &total), en = block_scan(sn, s.red2, &all);
+        const u64 need = need_of(total);
+        for (int i = 0; i < per; ++i) {
+            en += n[i];
+            if (at < need && need <= at + v[i]) {
+                s.found[0] = tid * per + i;
+                s.found[1] = need - at;
+                s.found[2] = n[i];
+                s.found[3] = en;
+            }
+            at += v[i];
+        }
+        all_sync();  // (the bins have been read everywhere)
+        return total;
+    };
+    // Elements with `take` go to CTA 0's list.
+    auto gather = [&](auto take) {
+        uint32_t* n = remote(&s.n_list, 0);
+        u64* list = remote(s.list, 0);
+        row.each([&](float x, int i) {
+            if (take(x, i)) list[atomicAdd(n, 1u)] = place(x, i);
+        });
+        all_sync();
+    };
+
+    // The cut of the shortest prefix, within what is kept, that reaches need_of(sum) elements or weight.
+    // True: the whole prefix is in CTA 0's list, sorted (n_list elements, some past it), and `total`
+    // is the sum that it is measured by; false: `cut` is set.
+    u64 total = 0;
+    auto find = [&](bool by_mass, auto need_of) {
+        const float range = by_mass ? 28.f * t_in : 64.f;  // (weights vanish 27.8 t below the maximum)
+        scale = kBins / fmaxf(fminf(top - bot, range), 0x1p-100f);
+        row.each([&](float x, int i) {
+            if (place(x, i) < cut) return;
+            const int b = bin_of(x);
+            if (by_mass) add_mass(b, weight(x));
+            atomicAdd(&s.cnt[b], 1u);
+        });
+        total = find_bin(by_mass, need_of);
+        const int bin = (int)s.found[0];
+        if (s.found[3] <= kList) {
+            const u64 kept = cut;
+            gather([&](float x, int i) { return bin_of(x) <= bin && place(x, i) >= kept; });
+            if (rank == 0) sort_list(s.list, (int)s.n_list, true);
+            return true;
+        }
+        u64 prefix = 0, need = s.found[1];
+        int shift = 32 + kIdxBits, width = 0;
+        while (s.found[2] > kList) {  // refine by the next bits of the place
+            width = shift > 11 ? 11 : shift;
+            shift -= width;
+            __syncthreads();
+            clear_bins();
+            __syncthreads();
+            row.each([&](float x, int i) {
+                const u64 c = place(x, i);
+                if (c < cut || bin_of(x) != bin || (c >> (shift + width)) != prefix) return;
+                // (bins ascend as the order does: the largest place first)
+                const int b = (1 << width) - 1 - (int)((c >> shift) & ((1u << width) - 1));
+                if (by_mass) add_mass(b, weight(x));
+                atomicAdd(&s.cnt[b], 1u);
+            });
+            find_bin(by_mass, [&](u64) { return need; });
+            prefix = prefix << width | (u64)((1 << width) - 1 - (int)s.found[0]);
+            need = s.found[1];
+        }
+        const u64 kept = cut;
+        gather([&](float x, int i) {
+            const u64 c = place(x, i);
+            return c >= kept && bin_of(x) == bin && (shift == 32 + kIdxBits || (c >> shift) == prefix);
+        });
+        if (rank == 0) {
+            const int n = (int)s.n_list;
+            sort_list(s.list, n, true);
+            const int per = (n + nt - 1) / nt;
+            u64 sum = 0, all;
+            for (int i = tid * per; i < min(n, (tid + 1) * per); ++i)
+                sum += by_mass ? weight(place_logit(s.list[i])) : 1;
+            u64 at = block_scan(sum, s.red, &all);
+            for (int i = tid * per; i < min(n, (tid + 1) * per); ++i) {
+                const u64 v = by_mass ? weight(place_logit(s.list[i])) : 1;
+                if (at < need && need <= at + v)
+                    for (int r = 0; r < C; ++r) *remote(&s.cut, r) = s.list[i];
+                at += v;
+            }
+            if (tid == 0) s.n_list = 0;
+        }
+        __syncthreads();
+        clear_bins();
+        all_sync();
+        cut = s.cut;
+        return false;
+    };
+    bool in_list = false;
+    if (k < V) in_list = find(false, [&](u64) { return (u64)k; });
+    if (use_p && !in_list)
+        in_list = find(true, [&](u64 sum) { return max((u64)1, part(sum, pf)); });
+
+    if (in_list) {  // CTA 0 has all that can be kept
+        if (rank != 0) return;
+        int n = (int)s.n_list;
+        const bool by_k = k < V;
+        if (by_k) n = min(n, (int)k);
+        const int per = (kList + nt - 1) / nt;
+        u64 w[8], sum = 0, all;
+        const int j0 = tid * per;
+        for (int i = 0; i < per; ++i) {
+            w[i] = j0 + i < n ? weight(place_logit(s.list[j0 + i])) : 0;
+            sum += w[i];
+        }
+        u64 at = block_scan(sum, s.red, &all);
+        const bool second = cut != 0;  // the list is top-p's, of what top-k kept
+        const u64 target = !use_p ? ~(u64)0
+                                  : max((u64)1, part(by_k && !second ? all : total, pf));
+        // kept: a prefix whose weights before it are short of the target, at least floor_w (the first
+        // always is: its weight is the largest)
+        int kept = 0;
+        for (int i = 0; i < per; ++i) {
+            if (j0 + i < n && at < target && (w[i] >= floor_w)) ++kept;
+            at += w[i];
+        }
+        u64 n_kept;
+        block_scan((u64)kept, s.red2, &n_kept);
+        n = (int)n_kept;
+        __syncthreads();
+        // by the index
+        for (int i = tid; i < n; i += nt) {
+            const u64 c = s.list[i];
+            s.list[i] = (u64)place_index(c) << 32 | (c >> kIdxBits);
+        }
+        __syncthreads();
+        sort_list(s.list, n, false);
+        sum = 0;
+        for (int i = 0; i < per; ++i) {
+            w[i] = j0 + i < n ? weight(logit_of((uint32_t)s.list[j0 + i])) : 0;
+            sum += w[i];
+        }
+        at = block_scan(sum, s.red, &all);
+        const u64 draw = part(all, uf);
+        for (int i = 0; i < per; ++i) {
+            if (at <= draw && draw < at + w[i]) {
+                p.out[m] = (int32_t)(s.list[j0 + i] >> 32);
+                if (p.p_out) p.p_out[m] = (float)w[i] / (float)all;
+            }
+            at += w[i];
+        }
+        return;
     }
-    // kept weights in the order of the index: each thread a run of indices
-    const int per = (V + kThreads - 1) / kThreads, i0 = min(V, tid * per), i1 = min(V, i0 + per);
-    auto scan = [&](u64 v, u64* total) {  // exclusive prefix over the block
-        u64 s = v;
+
+    // ---- the kept weights in the order of the index: a run of chunks per warp ----
+    constexpr int kPer = Row<DT>::kPer;
+    auto kept_weight = [&](float x, int i) {
+        if (place(x, i) < cut) return (u64)0;
+        const u64 w = weight(x);
+        return w >= floor_w ? w : (u64)0;
+    };
+    const int chunks = (row.n + kPer - 1) / kPer, warps = nt >> 5;
+    const int run = ((chunks + warps - 1) / warps + 31) / 32 * 32;  // chunks of a warp
+    u64 sum = 0;
+    for (int c = warp * run + lane; c < min(chunks, (warp + 1) * run); c += 32) {
+        float x[kPer];
+        Logits<DT>::unpack(row.raw(c), x);
 #pragma unroll
-        for (int o = 1; o < 32; o *= 2) {
-            const u64 y = __shfl_up_sync(0xffffffffu, s, o);
-            if ((tid & 31) >= o) s += y;
-        }
-        __syncthreads();
-        if ((tid & 31) == 31) red[tid >> 5] = s;
-        __syncthreads();
-        u64 before = 0, all = 0;
-        for (int j = 0; j < 32; ++j) {
-            if (j < (tid >> 5)) before += red[j];
-            all += red[j];
-        }
-        *total = all;
-        return before + s - v;
+        for (int e = 0; e < kPer; ++e)
+            if (kPer * c + e < row.n) sum += kept_weight(clean(x[e]), row.i0 + kPer * c + e);
+    }
+    u64 mine;
+    block_scan(sum, s.red, &mine);  // (red: the warps' sums)
+    if (tid < C) remote(s.sums, tid)[rank] = mine;
+    all_sync();
+    u64 all = 0, before = 0;
+    for (int r = 0; r < C; ++r) {
+        if (r < rank) before += s.sums[r];
+        all += s.sums[r];
+    }
+    const u64 draw = part(all, uf);
+    if (draw < before || draw >= before + mine) return;
+    // the warp whose run has it; the whole CTA looks through that run
+    int w0 = 0;
+    for (; w0 < warps - 1 && before + s.red[w0] <= draw; ++w0) before += s.red[w0];
+    const int e0 = w0 * run * kPer, e1 = min(row.n, (w0 + 1) * run * kPer);
+    const int per = (e1 - e0 + nt - 1) / nt;
+    sum = 0;
+    auto at_index = [&](int i) {
+        float x;
+        const uint32_t v = Logits<DT>::raw(row.src, i);
+        if (DT == LAQ_F32) x = __uint_as_float(v);
+        else if (DT == LAQ_F16) x = __half2float(__ushort_as_half((unsigned short)v));
+        else x = __uint_as_float(v << 16);
+        return kept_weight(clean(x), row.i0 + i);
     };
-    u64 eq = 0, all;
-    if (cut_on)
-        for (int i = i0; i < i1; ++i) eq += key_of(load_logit<DT>(row, i)) == cut.key;
-    const u64 eq0 = scan(eq, &all);
-    auto kept = [&](int i, u64& seen) {
-        const float x = load_logit<DT>(row, i);
-        const uint32_t key = key_of(x);
-        bool on = !cut_on || key > cut.key;
-        if (cut_on && key == cut.key) on = seen++ < cut.count;
-        const u64 w = on ? weight(x, top, t) : 0;
-        return w >= floor_w ? w : 0;
-    };
-    u64 s = 0, seen = eq0, total;
-    for (int i = i0; i < i1; ++i) s += kept(i, seen);
-    u64 before = scan(s, &total);
-    const u64 target = part(total, uf);
-    if (before <= target && target < before + s) {
-        seen = eq0;
-        for (int i = i0; i < i1; ++i) {
-            const u64 w = kept(i, seen);
-            before += w;
-            if (before > target) {
-                p.out[m] = i;
-                if (p.p_out) p.p_out[m] = (float)w / (float)total;
+    for (int i = e0 + tid * per; i < min(e1, e0 + (tid + 1) * per); ++i) sum += at_index(i);
+    u64 run_sum;
+    before += block_scan(sum, s.red2, &run_sum);
+    if (before <= draw && draw < before + sum)
+        for (int i = e0 + tid * per; i < min(e1, e0 + (tid + 1) * per); ++i) {
+            const u64 w = at_index(i);
+            if (draw < before + w) {
+                p.out[m] = row.i0 + i;
+                if (p.p_out) p.p_out[m] = (float)w / (float)all;
                 break;
             }
+            before += w;
         }
-    }
 }
 
+constexpr int kSliceBytes = 180 * 1024;  // beside SampleSmem in an SM's 227 KB
+
 template <int DT>
-laq_status launch_sample(const SampleParams& p, int64_t M, void* stream) {
+laq_status launch_sample(SampleParams p, int64_t M, void* stream) {
+    static std::atomic<int> sms_of[kMaxDevices];
+    const void* fn = (const void*)sample_kernel<DT>;
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return LAQ_ERR_CUDA;
+    int sms = sms_of[dev].load();
+    if (sms == 0) {
+        if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess ||
+            cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                 (int)sizeof(SampleSmem) + kSliceBytes) != cudaSuccess)
+            return LAQ_ERR_CUDA;
+        sms_of[dev].store(sms);
+    }
+    const int size = Logits<DT>::kSize;
+    int C = 1;
+    auto slice_of = [&](int c) { return (int)((((int64_t)p.V + c - 1) / c + 7) / 8 * 8); };
+    while (C < kMaxC && ((int64_t)slice_of(C) * size > kSliceBytes ||
+                         (M * C * 2 <= sms && slice_of(C) > 4096)))
+        C *= 2;
+    p.C = C;
+    p.slice = slice_of(C);
+    p.resident = (int64_t)p.slice * size <= kSliceBytes;
+    const int threads = p.slice > 8192 ? 1024 : p.slice > 2048 ? 512 : 256;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)M);
-    cfg.blockDim = dim3(kThreads);
+    cfg.gridDim = dim3((unsigned)(M * C));
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = sizeof(SampleSmem) + (p.resident ? (size_t)p.slice * size : 0);
     cfg.stream = static_cast<cudaStream_t>(stream);
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)C;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = C > 1 ? 2 : 1;
     return cudaLaunchKernelEx(&cfg, sample_kernel<DT>, p) == cudaSuccess ? LAQ_OK : LAQ_ERR_CUDA;
 }
 
@@ -246,7 +640,7 @@ extern "C" laq_status laq_sample(const void* logits, int32_t dtype, int64_t M, i
                                  const int32_t* top_k, const float* top_p, const float* min_p,
                                  const float* u, int32_t* out, float* p_out, void* stream) {
     if (dtype != LAQ_F16 && dtype != LAQ_BF16 && dtype != LAQ_F32) return LAQ_ERR_CONFIG;
-    if (M < 0 || M > 65535 || V < 1 || V > (int64_t)1 << 22 || row_stride < V ||
+    if (M < 0 || M > 65535 || V < 1 || V > (int64_t)1 << kIdxBits || row_stride < V ||
         row_stride > (int64_t)1 << 40)
         return LAQ_ERR_SHAPE;
     if (M == 0) return LAQ_OK;
@@ -255,8 +649,17 @@ extern "C" laq_status laq_sample(const void* logits, int32_t dtype, int64_t M, i
         (((uintptr_t)temperature | (uintptr_t)top_k | (uintptr_t)top_p | (uintptr_t)min_p |
           (uintptr_t)u | (uintptr_t)out | (uintptr_t)p_out) & 3u))
         return LAQ_ERR_ALIGN;
-    const SampleParams p = {logits, temperature, top_p, min_p, u, top_k, out, p_out, row_stride,
-                            (int)V};
+    SampleParams p = {};
+    p.logits = logits;
+    p.temperature = temperature;
+    p.top_p = top_p;
+    p.min_p = min_p;
+    p.u = u;
+    p.top_k = top_k;
+    p.out = out;
+    p.p_out = p_out;
+    p.row_stride = row_stride;
+    p.V = (int)V;
     if (dtype == LAQ_F32) return launch_sample<LAQ_F32>(p, M, stream);
     if (dtype == LAQ_BF16) return launch_sample<LAQ_BF16>(p, M, stream);
     return launch_sample<LAQ_F16>(p, M, stream);

@@ -154,3 +154,54 @@ def test_strided_rows_and_another_batch():
     a = _lib.laq_sample(x[:, :V], dev, stream=s)
     s.synchronize()
     assert torch.equal(a, _lib.laq_sample(x[:, :V], dev))
+
+
+def defined(x, u, t, k, p, m):
+    """The definition in whole numbers, step by step, with the device's expf and division."""
+    x = x.float()
+    x = torch.where(torch.isnan(x), torch.full_like(x, float("-inf")), x)
+    top = x.amax(1, keepdim=True)
+    c = lambda a, d: torch.as_tensor(np.asarray(a, d)).cuda()[:, None]
+    t, k, p, m, u = c(t, np.float32), c(k, np.int64), c(p, np.float32), c(m, np.float32), c(u, np.float32)
+    w = (torch.where(x == top, 1.0, torch.exp((x - top) / t)) * 2.0 ** 40).long()
+    by = torch.sort(x, dim=1, descending=True, stable=True).indices
+    ws, rank = w.gather(1, by), torch.arange(x.shape[1], device="cuda")[None]
+
+    def part(mass, f):
+        f = (f * 2.0 ** 24).long()
+        return (mass >> 24) * f + (((mass & 0xffffff) * f) >> 24)
+    keep = (k <= 0) | (rank < k)
+    ws = ws * keep
+    cum = ws.cumsum(1)
+    keep &= (p >= 1) | (rank == 0) | (cum - ws < part(cum[:, -1:], p))
+    keep &= (ws >= (m * 2.0 ** 40).long()) | (rank == 0)
+    w = w * torch.zeros_like(keep).scatter_(1, by, keep)
+    cum = w.cumsum(1)
+    tok = (cum <= part(cum[:, -1:], u)).sum(1)
+    return tok.cpu().numpy(), (w.gather(1, tok[:, None]).float() / cum[:, -1:].float())[:, 0].cpu().numpy()
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("M,V,stretch", [(70, 3001, 1.0), (40, 50000, 0.2), (12, 151936, 2.0),
+                                         (3, 300001, 1.0), (2, 1 << 22, 1.0), (9, 100000, 1e-3)])
+def test_every_step_is_exact(dtype, M, V, stretch):
+    """To the token and the bit of its probability: rows whose cut lies deep in the body of the
+    distribution, many logits of one value, cuts of thousands of tokens, nothing cut."""
+    rng = np.random.default_rng(V)
+    g = torch.Generator(device="cuda").manual_seed(V)
+    x = (stretch * torch.randn((M, V), generator=g, device="cuda")).to(TYPES[dtype])
+    x[::3, :: 7] = float("-inf")
+    x[1::3, 5] = stretch * 9
+    for settings in range(8):
+        t = np.exp(rng.uniform(-1.5, 1.5, M)).astype(np.float32)
+        t[0] = (1e-30, 1e30, 1.0, 3e38, 1e-38, 2.0 ** -100, 2.0 ** 100, 0.99999994)[settings]
+        k = rng.integers(2, [V + 5, 80][settings % 2], M) if settings & 1 or settings == 6 \
+            else np.zeros(M, int)
+        p = rng.random(M).astype(np.float32) if settings & 2 else np.ones(M, np.float32)
+        m = (0.1 * rng.random(M) ** 4).astype(np.float32) if settings & 4 else np.zeros(M, np.float32)
+        u = rng.random(M).astype(np.float32)
+        u[-1] = 1 - 2.0 ** -24
+        tok, prob = sample(x, u, t, k, p, m)
+        want, share = defined(x, u, t, k, p, m)
+        assert np.array_equal(tok, want), settings
+        assert np.array_equal(prob, share), settings
