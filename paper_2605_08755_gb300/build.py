@@ -17,7 +17,7 @@ BUILD_DIR = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "liblaq.so")
 SOURCES = ("laq_api.cu", "laq_quant.cu", "laq_gemm.cu", "laq_gemm_batch.cu",
            "laq_gemm_prologue.cu", "laq_chain.cu",
-           "laq_decode.cu", "laq_rotate.cu", "laq_pass.cu", "laq_paged.cu", "laq_paged_attn.cu", "laq_sample.cu")
+           "laq_decode.cu", "laq_rotate.cu", "laq_pass.cu", "laq_paged.cu", "laq_paged_attn.cu", "laq_paged_decode.cu", "laq_sample.cu")
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

@@ -2,6 +2,8 @@
 // norms and the rotation, and the entry points of the attention over the pages.
 #include <math.h>
 
+#include <atomic>
+
 #include "laq_device.cuh"
 #include "laq_paged.cuh"
 #include "laq_paged_attn.cuh"
@@ -43,6 +45,51 @@ laq_status paged_kv(const laq_paged_kv* kv, int64_t T, int32_t Hq, PagedKv* out)
     o.Hkv = kv->Hkv;
     *out = o;
     return LAQ_OK;
+}
+
+namespace {
+
+typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*,
+                                const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                                const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiled encode_tiled() {
+    static std::atomic<EncodeTiled> fn{nullptr};
+    EncodeTiled f = fn.load();
+    if (!f) {
+        void* e = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &e, 12000, cudaEnableDefault,
+                                             &q) != cudaSuccess ||
+            q != cudaDriverEntryPointSuccess)
+            return nullptr;
+        f = reinterpret_cast<EncodeTiled>(e);
+        fn.store(f);
+    }
+    return f;
+}
+
+}  // namespace
+
+bool encode_map(CUtensorMap* m, bool bf, int rank, const void* base, const cuuint64_t* dims,
+                const cuuint64_t* strides, const cuuint32_t* box) {
+    const EncodeTiled f = encode_tiled();
+    const cuuint32_t one[4] = {1, 1, 1, 1};
+    return f && f(m, bf ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16,
+                  (cuuint32_t)rank, const_cast<void*>(base), dims, strides, box, one,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                  CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+bool encode_cache(CUtensorMap* m, const PagedKv& kv, bool bf, const void* base, int rows) {
+    const cuuint64_t dims[4] = {kPagedDim, (cuuint64_t)1 << kv.page_bits, (cuuint64_t)kv.Hkv,
+                                (cuuint64_t)kv.pages};
+    const cuuint64_t strides[3] = {(cuuint64_t)kv.token_stride * 2, (cuuint64_t)kv.head_stride * 2,
+                                   (cuuint64_t)kv.page_stride * 2};
+    const cuuint32_t box[4] = {64, (cuuint32_t)rows, 1, 1};
+    return encode_map(m, bf, 4, base, dims, strides, box);
 }
 
 namespace {
@@ -267,7 +314,8 @@ size_t laq_paged_attention_workspace_bytes(int64_t T, int64_t batch, int64_t max
     if (T < 0 || batch < 0 || max_q < 0 || T > most || batch > most || Hq < 1 || Hkv < 1 ||
         Hkv > 4096 || Hq % Hkv || Hq / Hkv > 64)
         return 0;
-    return chunk_workspace_bytes(max_q, Hq / Hkv);
+    return max_q * (Hq / Hkv) <= kDecodeRows ? decode_workspace_bytes(max_q, Hq / Hkv)
+                                             : chunk_workspace_bytes(max_q, Hq / Hkv);
 }
 
 laq_status laq_paged_attention(const laq_paged_kv* kv, const void* q, int64_t q_stride, int64_t T,
@@ -285,8 +333,9 @@ laq_status laq_paged_attention(const laq_paged_kv* kv, const void* q, int64_t q_
         workspace_bytes < laq_paged_attention_workspace_bytes(T, kv->batch, max_q, Hq, kv->Hkv))
         return LAQ_ERR_WORKSPACE;
     if (T == 0 || kv->batch == 0 || max_q == 0) return LAQ_OK;
-    return launch_chunk(o, kv->dtype == LAQ_BF16, q, q_stride, (int)T, (int)(max_q < T ? max_q : T),
-                        Hq, scale, out, workspace, static_cast<cudaStream_t>(stream));
+    const auto launch = max_q * (Hq / kv->Hkv) <= kDecodeRows ? launch_decode : launch_chunk;
+    return launch(o, kv->dtype == LAQ_BF16, q, q_stride, (int)T, (int)(max_q < T ? max_q : T), Hq,
+                  scale, out, workspace, static_cast<cudaStream_t>(stream));
 }
 
 }  // extern "C"

@@ -39,7 +39,6 @@ constexpr int kTileBytes = 2 * kHalf;
 constexpr int kStages = 5;              // K and V tiles in flight (160 KB)
 constexpr int kThreads = 320;           // 2 warpgroups of softmax, a TMA warp, an MMA warp
 constexpr int kSmemTiles = (2 + kStages) * kTileBytes;
-constexpr long long kWaitCycles = 2000000000;  // about a second
 constexpr float kGrow = 8.f;            // how far a maximum may grow before O is rescaled (log2)
 
 struct Bars {
@@ -53,57 +52,9 @@ struct Bars {
 };
 constexpr int kSmem = kSmemTiles + 1024 + (int)sizeof(Bars);
 
-__device__ __forceinline__ uint32_t s32(const void* p) {
-    return (uint32_t)__cvta_generic_to_shared(p);
-}
-__device__ __forceinline__ void bar_init(uint64_t* b, int n) {
-    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(s32(b)), "r"(n) : "memory");
-}
-__device__ __forceinline__ void bar_arrive(uint64_t* b) {
-    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(s32(b)) : "memory");
-}
-__device__ __forceinline__ void bar_expect(uint64_t* b, uint32_t bytes) {
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(s32(b)), "r"(bytes)
-                 : "memory");
-}
-__device__ __forceinline__ bool bar_try(uint64_t* b, uint32_t parity) {
-    uint32_t ok;
-    asm volatile(
-        "{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n"
-        "selp.u32 %0, 1, 0, p;\n}\n"
-        : "=r"(ok)
-        : "r"(s32(b)), "r"(parity)
-        : "memory");
-    return ok;
-}
-// Bounded wait; false once any wait of the CTA has run out (every role then leaves its loop).
-__device__ __forceinline__ bool bar_wait(Bars* s, uint64_t* b, uint32_t parity) {
-    if (bar_try(b, parity)) return true;
-    const long long t0 = clock64();
-    do {
-        if (bar_try(b, parity)) return true;
-        if (*(volatile uint32_t*)&s->abort) return false;
-    } while (clock64() - t0 < kWaitCycles);
-    *(volatile uint32_t*)&s->abort = 1;
-    return false;
-}
 // The same for a whole warp, which stays together.
 __device__ __forceinline__ bool warp_wait(Bars* s, uint64_t* b, uint32_t parity) {
-    return __all_sync(0xffffffffu, bar_wait(s, b, parity));
-}
-// For what is in flight when a wait has run out.
-__device__ __forceinline__ void drain(uint64_t* b, uint32_t parity) {
-    const long long t0 = clock64();
-    while (!bar_try(b, parity) && clock64() - t0 < kWaitCycles) {
-    }
-}
-__device__ __forceinline__ void tma4(uint32_t dst, const CUtensorMap* m, int c0, int c1, int c2,
-                                     int c3, uint64_t* bar) {
-    asm volatile(
-        "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], "
-        "[%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
-        "l"(m), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(s32(bar))
-        : "memory");
+    return __all_sync(0xffffffffu, bar_wait(&s->abort, b, parity));
 }
 __device__ __forceinline__ void tma3(uint32_t dst, const CUtensorMap* m, int c0, int c1, int c2,
                                      uint64_t* bar) {
@@ -177,11 +128,6 @@ __device__ __forceinline__ void tm_wait_ld() {
 }
 __device__ __forceinline__ void tm_wait_st() {
     asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
-}
-__device__ __forceinline__ float ex2(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
 }
 // Pins loaded values behind the wait that makes them valid.
 __device__ __forceinline__ void pin32(float* r) {
@@ -295,11 +241,6 @@ struct Walk {
         return false;
     }
 };
-
-// The CTA whose share has unit u: shares start at floor(c W / ctas).
-__device__ __forceinline__ int cta_of(long long u, long long W, int ctas) {
-    return (int)(((u + 1) * ctas - 1) / W);
-}
 
 // Every thread takes a run of requests; one of them finds where the CTA's share starts.
 __device__ void plan(const ChunkParams& p, Bars* s) {
@@ -458,7 +399,7 @@ __device__ void mma_role(const ChunkParams& p, Bars* s, uint32_t smem, uint32_t 
     uint32_t use = 0, pieces = 0, np[2] = {0, 0};
     auto stage = [&](uint32_t f) { return smem + (2 + f % kStages) * kTileBytes; };
     auto wait_full = [&](uint32_t f) {
-        return bar_wait(s, &s->full[f % kStages], (f / kStages) & 1);
+        return bar_wait(&s->abort, &s->full[f % kStages], (f / kStages) & 1);
     };
     auto qk = [&](int i, int qt, uint32_t f) {
         const uint32_t q = smem + qt * kTileBytes, k = stage(f);
@@ -476,12 +417,12 @@ __device__ void mma_role(const ChunkParams& p, Bars* s, uint32_t smem, uint32_t 
             mma_ts(tmem + 256 + 128 * i, tmem + 128 * i + 8 * kk, vdesc(v + kk * 2048), kPv,
                    kk > 0 || !first);
     };
-    auto wait_p = [&](int i) { return bar_wait(s, &s->p_full[i], np[i]++ & 1); };
+    auto wait_p = [&](int i) { return bar_wait(&s->abort, &s->p_full[i], np[i]++ & 1); };
     bool ok = true;
     while (ok && w.next(x)) {
         if (x.nt == 0) continue;
         const bool narrow = x.ntok <= p.tau;
-        if (!bar_wait(s, &s->q_full, pieces & 1)) break;
+        if (!bar_wait(&s->abort, &s->q_full, pieces & 1)) break;
         ++pieces;
         const int n = x.hi - x.lo;
         if (!narrow) {
@@ -634,11 +575,18 @@ __device__ void softmax_role(const ChunkParams& p, Bars* s, uint32_t tmem) {
         }
         const int seen = x.pos0 + (valid ? r_item / p.G : 0) + 1;     // tokens this row sees
         const int least = x.pos0 + (narrow ? 0 : wg * p.tau) + 1;    // .. the tile's first row sees
+        const bool busy = __any_sync(0xffffffffu, valid);  // (other warps only keep the order)
         float m = -INFINITY, l = 0.f;
         bool first = true;
         for (int j = x.lo + (narrow ? wg : 0); j < x.hi; j += narrow ? 2 : 1) {
             if (!(ok = warp_wait(s, &s->s_full[wg], ns++ & 1))) break;
             tc_after();
+            if (!busy) {
+                first = false;
+                tc_before();
+                if ((threadIdx.x & 31) == 0) bar_arrive(&s->p_full[wg]);
+                continue;
+            }
             float v[128];
 #pragma unroll
             for (int q = 0; q < 4; ++q) tm_ld32(ts + 32 * q, v + 32 * q);
@@ -702,7 +650,7 @@ __device__ void softmax_role(const ChunkParams& p, Bars* s, uint32_t tmem) {
             if (!(ok = warp_wait(s, &s->o_full[wg], no++ & 1))) break;
             tc_after();
             const float inv = l == 0.f ? 0.f : 1.f / l;
-            for (int q = 0; q < 4; ++q) {
+            for (int q = 0; busy && q < 4; ++q) {
                 float o[32];
                 tm_ld32(to + 32 * q, o);
                 tm_wait_ld();
@@ -819,40 +767,6 @@ __global__ void __launch_bounds__(kThreads, 1) paged_chunk_kernel(
     if (threadIdx.x == 0 && s->abort) atomicExch(p.status, (uint32_t)LAQ_ERR_TIMEOUT);
 }
 
-typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*,
-                                const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
-                                const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-EncodeTiled encode_tiled() {
-    static std::atomic<EncodeTiled> fn{nullptr};
-    EncodeTiled f = fn.load();
-    if (!f) {
-        void* e = nullptr;
-        cudaDriverEntryPointQueryResult q;
-        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &e, 12000, cudaEnableDefault,
-                                             &q) != cudaSuccess ||
-            q != cudaDriverEntryPointSuccess)
-            return nullptr;
-        f = reinterpret_cast<EncodeTiled>(e);
-        fn.store(f);
-    }
-    return f;
-}
-
-bool encode(CUtensorMap* m, bool bf, int rank, const void* base, const cuuint64_t* dims,
-            const cuuint64_t* strides, const cuuint32_t* box) {
-    const EncodeTiled f = encode_tiled();
-    const cuuint32_t one[4] = {1, 1, 1, 1};
-    return f && f(m, bf ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16,
-                  (cuuint32_t)rank, const_cast<void*>(base), dims, strides, box, one,
-                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-                  CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
-constexpr int kMaxCtas = 256;
-constexpr size_t kHeader = 4096;  // status, counters
 
 int part_rows(int64_t max_q, int G) {
     const int64_t per = 128 / G * G, rows = max_q * G;
@@ -862,8 +776,8 @@ int part_rows(int64_t max_q, int G) {
 }  // namespace
 
 size_t chunk_workspace_bytes(int64_t max_q, int G) {
-    const size_t rows = (size_t)kMaxCtas * 4 * part_rows(max_q, G);
-    return kHeader + rows * (kPagedDim * sizeof(float) + sizeof(float2));
+    const size_t rows = (size_t)kPartCtas * 4 * part_rows(max_q, G);
+    return kPartHeader + rows * (kPagedDim * sizeof(float) + sizeof(float2));
 }
 
 laq_status launch_chunk(const PagedKv& kv, bool bf, const void* q, int64_t q_stride, int T, int max_q,
@@ -880,7 +794,7 @@ laq_status launch_chunk(const PagedKv& kv, bool bf, const void* q, int64_t q_str
             cudaFuncSetAttribute((const void*)paged_chunk_kernel<false>,
                                  cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem) != cudaSuccess)
             return LAQ_ERR_CUDA;
-        if (sms > kMaxCtas) sms = kMaxCtas;
+        if (sms > kPartCtas) sms = kPartCtas;
         sms_of[dev].store(sms);
     }
     ChunkParams p = {};
@@ -896,21 +810,17 @@ laq_status launch_chunk(const PagedKv& kv, bool bf, const void* q, int64_t q_str
     p.out = static_cast<uint16_t*>(out);
     uint8_t* ws = static_cast<uint8_t*>(workspace);
     p.status = reinterpret_cast<uint32_t*>(ws);
-    p.count = p.status + 64;
-    p.done = p.count + kMaxCtas;
-    const size_t rows = (size_t)kMaxCtas * 4 * p.part_rows;
-    p.part = reinterpret_cast<float*>(ws + kHeader);
+    p.count = p.status + kCountAt;
+    p.done = p.status + kDoneAt;
+    const size_t rows = (size_t)kPartCtas * 4 * p.part_rows;
+    p.part = reinterpret_cast<float*>(ws + kPartHeader);
     p.ml = reinterpret_cast<float2*>(p.part + rows * kPagedDim);
     const int P = 1 << kv.page_bits, box = P < kTile ? P : kTile;
-    const cuuint64_t kd[4] = {kPagedDim, (cuuint64_t)P, (cuuint64_t)kv.Hkv, (cuuint64_t)kv.pages};
-    const cuuint64_t ks[3] = {(cuuint64_t)kv.token_stride * 2, (cuuint64_t)kv.head_stride * 2,
-                              (cuuint64_t)kv.page_stride * 2};
-    const cuuint32_t kb[4] = {64, (cuuint32_t)box, 1, 1};
     const cuuint64_t qd[3] = {kPagedDim, (cuuint64_t)Hq, (cuuint64_t)T};
     const cuuint64_t qs[2] = {kPagedDim * 2, (cuuint64_t)q_stride * 2};
     const cuuint32_t qb[3] = {64, (cuuint32_t)p.G, (cuuint32_t)p.tau};
-    if (!encode(&p.kmap, bf, 4, kv.k, kd, ks, kb) || !encode(&p.vmap, bf, 4, kv.v, kd, ks, kb) ||
-        !encode(&p.qmap, bf, 3, q, qd, qs, qb))
+    if (!encode_cache(&p.kmap, kv, bf, kv.k, box) || !encode_cache(&p.vmap, kv, bf, kv.v, box) ||
+        !encode_map(&p.qmap, bf, 3, q, qd, qs, qb))
         return LAQ_ERR_CUDA;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)sms);

@@ -7,6 +7,12 @@
 
 namespace laq {
 
+constexpr int kPartCtas = 256;        // CTAs of the chunk kernel that the workspace has room for
+constexpr size_t kPartHeader = 8192;  // bytes: status, counters
+// Calls of up to this many rows (new tokens x q heads) per kv head run the decode kernel.
+constexpr int kDecodeRows = 16;
+constexpr int kCountAt = 64, kDoneAt = 64 + 1024;  // words of the header
+
 // paged_chunk_kernel's parameter (see laq_paged_attn.cu)
 struct ChunkParams {
     CUtensorMap qmap, kmap, vmap;
@@ -23,4 +29,78 @@ size_t chunk_workspace_bytes(int64_t max_q, int G);
 laq_status launch_chunk(const PagedKv& kv, bool bf, const void* q, int64_t q_stride, int T, int max_q,
                         int Hq, float scale, void* out, void* workspace, cudaStream_t stream);
 
+size_t decode_workspace_bytes(int64_t max_q, int G);
+laq_status launch_decode(const PagedKv& kv, bool bf, const void* q, int64_t q_stride, int T,
+                         int max_q, int Hq, float scale, void* out, void* workspace,
+                         cudaStream_t stream);
+
+// A tiled TMA map of a 16-bit tensor with the 128-byte swizzle (rank 3 or 4; strides in bytes).
+bool encode_map(CUtensorMap* m, bool bf, int rank, const void* base, const cuuint64_t* dims,
+                const cuuint64_t* strides, const cuuint32_t* box);
+// The map of a cache's k or v with boxes of `rows` slots of 64 elements.
+bool encode_cache(CUtensorMap* m, const PagedKv& kv, bool bf, const void* base, int rows);
+
+namespace {
+
+constexpr long long kWaitCycles = 2000000000;  // about a second
+
+__device__ __forceinline__ uint32_t s32(const void* p) {
+    return (uint32_t)__cvta_generic_to_shared(p);
+}
+__device__ __forceinline__ void bar_init(uint64_t* b, int n) {
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(s32(b)), "r"(n) : "memory");
+}
+__device__ __forceinline__ void bar_arrive(uint64_t* b) {
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(s32(b)) : "memory");
+}
+__device__ __forceinline__ void bar_expect(uint64_t* b, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(s32(b)), "r"(bytes)
+                 : "memory");
+}
+__device__ __forceinline__ bool bar_try(uint64_t* b, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n"
+        "selp.u32 %0, 1, 0, p;\n}\n"
+        : "=r"(ok)
+        : "r"(s32(b)), "r"(parity)
+        : "memory");
+    return ok;
+}
+// Bounded wait; false once any wait of the CTA has run out (*abort: its flag in shared memory).
+__device__ __forceinline__ bool bar_wait(uint32_t* abort, uint64_t* b, uint32_t parity) {
+    if (bar_try(b, parity)) return true;
+    const long long t0 = clock64();
+    do {
+        if (bar_try(b, parity)) return true;
+        if (*(volatile uint32_t*)abort) return false;
+    } while (clock64() - t0 < kWaitCycles);
+    *(volatile uint32_t*)abort = 1;
+    return false;
+}
+// For what is in flight when a wait has run out.
+__device__ __forceinline__ void drain(uint64_t* b, uint32_t parity) {
+    const long long t0 = clock64();
+    while (!bar_try(b, parity) && clock64() - t0 < kWaitCycles) {
+    }
+}
+__device__ __forceinline__ void tma4(uint32_t dst, const CUtensorMap* m, int c0, int c1, int c2,
+                                     int c3, uint64_t* bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], "
+        "[%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
+        "l"(m), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(s32(bar))
+        : "memory");
+}
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__host__ __device__ // The CTA whose share has unit u: shares start at floor(c W / ctas).
+__device__ __forceinline__ int cta_of(long long u, long long W, int ctas) {
+    return (int)(((u + 1) * ctas - 1) / W);
+}
+
+}  // namespace
 }  // namespace laq

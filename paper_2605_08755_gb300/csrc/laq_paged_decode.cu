@@ -1,0 +1,538 @@
+// laq_paged_decode.cu -- attention of a few new tokens per request over the paged cache: up to 16 rows
+// (new tokens x q heads of a kv head), where reading K and V is what counts.
+//
+// A pair is (request, kv head).  CTAs of 8 warps, two per SM, walk equal shares of all pairs' tokens in
+// order, in units of 128 tokens; within a CTA's part of a pair the warps take steps of 16 tokens in
+// turn.  A warp streams its steps' K and V (4 KB each, one TMA box per page and 64 dimensions) through a
+// ring of kSlots slots of its own and keeps the running maximum, sum and output of its tokens
+// for the rows at once (m16n8k16, fp32 accumulation):
+//   S^T = K q^T: A the K rows from ldmatrix, B the rows of q, loaded once into registers;
+//   O^T += V^T P^T: A from ldmatrix.trans, B the probabilities after a movmatrix transpose.
+// P is rounded once to the cache's type (in units of 2^7 over the row's maximum in fp16, so that small
+// ones stay normal); its sum is of the rounded values' fp32 originals.  The 16 tokens of a step are
+// summed by the tensor cores from zero, which truncate what they add, and the steps in fp32 registers.
+// The maximum moves only when a row's has grown by 2^8 (all of a warp's rows then rescale).
+//   The warps meet in shared memory, each in its own ring.  A pair that a share's border cuts is added
+// up by the last of its CTAs to finish, from the parts in the workspace in their order.
+#include <cuda.h>
+#include <math.h>
+
+#include <atomic>
+
+#include "laq_device.cuh"
+#include "laq_internal.cuh"
+#include "laq_paged_attn.cuh"
+
+namespace laq {
+namespace {
+
+constexpr int kWarps = 8;
+constexpr int kThreads = kWarps * 32;
+constexpr int kSlots = 3;
+constexpr int kStep = 16;                     // tokens
+constexpr int kSlotBytes = kStep * 256;       // K or V of a step: two halves of 64 dimensions
+constexpr int kUnit = kStep * kWarps;         // tokens
+constexpr int kRow = kPagedDim + 4;           // floats of a row while the warps meet
+constexpr float kGrow = 8.f;
+constexpr int kMaxParts = 2 * kPartCtas;      // CTAs
+
+struct DecodeParams {
+    CUtensorMap kmap, vmap;
+    PagedKv kv;
+    const uint16_t* q;
+    uint16_t* out;
+    float* part;   // [CTA][2 slots][rows][D]
+    float2* ml;
+    uint32_t *status, *count;
+    int64_t q_stride;
+    int G, Hq, T, max_q, part_rows;
+    float scale_log2;
+};
+
+struct DecodeSmem {
+    float2 wml[kWarps][kDecodeRows];
+    float weight[kWarps][kDecodeRows];
+    float2 ml[kDecodeRows];
+    uint64_t full[kWarps][kSlots];
+    uint32_t abort;
+    int b, g, last;
+    long long at, u0, u1, W, scan[kWarps];
+    int ctas;
+};
+constexpr int kRing = kWarps * kSlots * kSlotBytes;
+constexpr int kSmem = kRing + 1024 + (int)sizeof(DecodeSmem);
+
+__device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t (&r)[4]) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];\n"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+                 : "r"(addr)
+                 : "memory");
+}
+__device__ __forceinline__ void ldsm4t(uint32_t addr, uint32_t (&r)[4]) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];\n"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+                 : "r"(addr)
+                 : "memory");
+}
+__device__ __forceinline__ uint32_t movmatrix(uint32_t v) {
+    uint32_t r;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;\n" : "=r"(r) : "r"(v));
+    return r;
+}
+template <bool BF>
+__device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0,
+                                    uint32_t b1) {
+    if (BF)
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, "
+            "{%8,%9}, {%0,%1,%2,%3};\n"
+            : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+            : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+    else
+        mma16816(d, a[0], a[1], a[2], a[3], b0, b1);
+}
+
+// Units of a request's pairs: one where it has rows but no tokens (zeros are to be written).
+struct Request {
+    int s0, n, past, len;
+    __device__ void load(const DecodeParams& p, int b) {
+        s0 = p.kv.q_start[b];
+        const int all = p.kv.q_start[b + 1] - s0;
+        len = min(max(p.kv.kv_len[b], 0), p.kv.max_tokens);
+        past = len - all;
+        n = s0 < 0 || s0 >= p.T || all <= 0 ? 0 : min(min(all, p.max_q), p.T - s0);
+    }
+    __device__ int units() const { return n == 0 ? 0 : max(1, (len + kUnit - 1) / kUnit); }
+};
+
+// Where this CTA's share starts: its units u0 .. u1 - 1 of W, and the pair that u0 is in (its first
+// unit: at).
+__device__ void plan(const DecodeParams& p, DecodeSmem* s) {
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int per = (p.kv.batch + kThreads - 1) / kThreads;
+    const int b0 = min(p.kv.batch, tid * per), b1 = min(p.kv.batch, b0 + per);
+    Request r;
+    long long sum = 0;
+    for (int b = b0; b < b1; ++b) {
+        r.load(p, b);
+        sum += (long long)r.units() * p.kv.Hkv;
+    }
+    long long inc = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o *= 2) {
+        const long long y = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += y;
+    }
+    if (lane == 31) s->scan[warp] = inc;
+    if (tid == 0) s->u0 = s->u1 = 0;
+    __syncthreads();
+    long long before = 0, W = 0;
+    for (int k = 0; k < kWarps; ++k) {
+        if (k < warp) before += s->scan[k];
+        W += s->scan[k];
+    }
+    before += inc - sum;
+    const int ctas = (int)min((long long)gridDim.x, W);
+    if ((int)blockIdx.x >= ctas) return;
+    const long long u0 = W * blockIdx.x / ctas;
+    if (u0 < before || u0 >= before + sum) return;
+    int b = b0;
+    long long at = before;
+    int units = 0;
+    for (; b < b1; ++b) {
+        r.load(p, b);
+        units = r.units();
+        if (u0 < at + (long long)units * p.kv.Hkv) break;
+        at += (long long)units * p.kv.Hkv;
+    }
+    s->b = b;
+    s->g = (int)((u0 - at) / units);
+    s->at = at + (long long)s->g * units;
+    s->u0 = u0;
+    s->u1 = W * (blockIdx.x + 1) / ctas;
+    s->W = W;
+    s->ctas = ctas;
+}
+
+template <bool BF, int NT>
+__global__ void __launch_bounds__(kThreads, 2) paged_decode_kernel(
+    const __grid_constant__ DecodeParams p) {
+    using H = Half16<BF>;
+    extern __shared__ uint8_t raw[];
+    const uint32_t ring = (s32(raw) + 1023u) & ~1023u;
+    uint8_t* ring_ptr = raw + (ring - s32(raw));
+    DecodeSmem* s = reinterpret_cast<DecodeSmem*>(ring_ptr + kRing);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, c = lane & 3, r8 = lane >> 2;
+    pdl_launch_dependents();
+    if (tid == 0) {
+        for (int w = 0; w < kWarps; ++w)
+            for (int i = 0; i < kSlots; ++i) bar_init(&s->full[w][i], 1);
+        s->abort = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    pdl_wait();
+    plan(p, s);
+    __syncthreads();
+    const int P = 1 << p.kv.page_bits, box = min(P, kStep);
+    const uint32_t slots = ring + warp * kSlots * kSlotBytes;
+    uint32_t seq = 0, issued = 0;  // K, V, K, V .. of the warp's steps: used and asked for so far
+    int b = s->b, g = s->g;
+    long long at = s->at, u = s->u0;
+    const long long u1 = s->u1;
+    Request req;
+    if (u < u1) req.load(p, b);
+    while (u < u1) {
+        const int units = req.units();
+        const long long end = min(u1, at + units);
+        const int t0 = (int)(u - at) * kUnit, t1 = min(req.len, (int)(end - at) * kUnit);
+        const int steps = max(0, (t1 - t0 + kStep - 1) / kStep);
+        const int mine = (steps - warp + kWarps - 1) / kWarps;  // this warp's steps (<= 0: none)
+        const int rows = req.n * p.G;
+        const int32_t* table = p.kv.table + (int64_t)b * p.kv.table_stride;
+        // ---- the ring: lane 2 i + h asks for half h of the i-th page (box) of a step ----
+        auto page_of = [&](int i) {  // of step i of this warp
+            const int tok = t0 + (i * kWarps + warp) * kStep + (lane >> 1) * box;
+            return i < mine && (lane >> 1) * box < kStep && tok < t1
+                       ? table[tok >> p.kv.page_bits] : -1;
+        };
+        int page = page_of(0), page_next = 0;
+        int sent = 0;  // of this part: K, V, K, V ..
+        auto send = [&] {
+            const int i = sent >> 1;
+            if (i >= mine) return;
+            const int tok = t0 + (i * kWarps + warp) * kStep;
+            const int boxes = (min(kStep, t1 - tok) + box - 1) / box;
+            const uint32_t slot = issued % kSlots;
+            if (lane == 0) bar_expect(&s->full[warp][slot], boxes * box * 256);
+            if ((sent & 1) == 0) page_next = page_of(i + 1);
+            __syncwarp();
+            const int k = lane >> 1, h = lane & 1;
+            if (k < boxes)
+                tma4(slots + slot * kSlotBytes + h * (kStep * 128) + k * box * 128,
+                     (sent & 1) ? &p.vmap : &p.kmap, 64 * h, (tok + k * box) & (P - 1), g, page,
+                     &s->full[warp][slot]);
+            if (sent & 1) page = page_next;
+            ++sent;
+            ++issued;
+        };
+#pragma unroll
+        for (int i = 0; i < kSlots; ++i) send();
+        // ---- q: B fragments, row n = lane / 4 of each 8 rows ----
+        uint32_t qf[NT][16];
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+            const int row = 8 * j + r8;
+            const uint32_t* src = reinterpret_cast<const uint32_t*>(
+                p.q + (int64_t)(req.s0 + row / p.G) * p.q_stride +
+                (int64_t)(g * p.G + row % p.G) * kPagedDim);
+#pragma unroll
+            for (int k = 0; k < 16; ++k) qf[j][k] = row < rows ? src[4 * k + c] : 0u;
+        }
+        // tokens that the rows of this lane's accumulators (2c, 2c + 1 of each 8) see
+        int lim[NT][2];
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+                lim[j][e] = req.past + min(8 * j + 2 * c + e, rows - 1) / p.G + 1;
+        const int least = req.past + 1;
+        float m[NT][2], l[NT][2], o[NT][8][4];
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+            m[j][0] = m[j][1] = -INFINITY;
+            l[j][0] = l[j][1] = 0.f;
+#pragma unroll
+            for (int d = 0; d < 8; ++d)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[j][d][e] = 0.f;
+        }
+        const float offset = BF ? 0.f : 7.f;
+        bool ok = true;
+        for (int i = 0; i < mine; ++i) {
+            const int tok = t0 + (i * kWarps + warp) * kStep;
+            // ---- scores of 16 tokens ----
+            ok = __all_sync(0xffffffffu, bar_wait(&s->abort, &s->full[warp][seq % kSlots],
+                                                  (seq / kSlots) & 1));
+            if (!ok) break;
+            uint32_t base = slots + (seq % kSlots) * kSlotBytes;
+            float sc[NT][4] = {};
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {  // lanes 0-15: rows of dimensions 16k .. +7, 16-31: +8 .. 15
+                uint32_t a[4];
+                const int row = lane & 15, j = 2 * k + (lane >> 4);
+                ldsm4(base + (j >> 3) * (kStep * 128) + row * 128 + (((j & 7) ^ (row & 7)) << 4), a);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) mma<BF>(sc[n], a, qf[n][2 * k], qf[n][2 * k + 1]);
+            }
+            __syncwarp();
+            ++seq;
+            send();
+            // accumulators: (token r8, rows 2c, 2c+1), (token r8 + 8, ..)
+            if (tok + kStep > least) {
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (tok + r8 + 8 * (e >> 1) >= lim[n][e & 1]) sc[n][e] = -INFINITY;
+            }
+            float mx[NT][2];
+            bool grow = false;
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    float x = fmaxf(sc[n][e], sc[n][e + 2]);
+                    x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
+                    x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
+                    x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
+                    mx[n][e] = x;
+                    grow |= (x - m[n][e]) * p.scale_log2 > kGrow;  // (-inf - -inf: no)
+                }
+            if (__any_sync(0xffffffffu, grow)) {
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const float to = fmaxf(m[n][e], mx[n][e]);
+                        const float f = m[n][e] == -INFINITY ? 0.f : ex2((m[n][e] - to) * p.scale_log2);
+                        m[n][e] = to;
+                        l[n][e] *= f;
+#pragma unroll
+                        for (int d = 0; d < 8; ++d) {
+                            o[n][d][e] *= f;
+                            o[n][d][e + 2] *= f;
+                        }
+                    }
+            }
+            uint32_t pf[NT][2];
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                const float b0 = (m[n][0] == -INFINITY ? 0.f : m[n][0] * p.scale_log2) - offset;
+                const float b1 = (m[n][1] == -INFINITY ? 0.f : m[n][1] * p.scale_log2) - offset;
+                const float e0 = ex2(fmaf(sc[n][0], p.scale_log2, -b0)),
+                            e1 = ex2(fmaf(sc[n][1], p.scale_log2, -b1)),
+                            e2 = ex2(fmaf(sc[n][2], p.scale_log2, -b0)),
+                            e3 = ex2(fmaf(sc[n][3], p.scale_log2, -b1));
+                l[n][0] += e0 + e2;
+                l[n][1] += e1 + e3;
+                pf[n][0] = movmatrix(H::pack(e0, e1));  // k = tokens 2c, 2c + 1 of row r8
+                pf[n][1] = movmatrix(H::pack(e2, e3));  // .. + 8
+            }
+            // ---- the tokens' values ----
+            ok = __all_sync(0xffffffffu, bar_wait(&s->abort, &s->full[warp][seq % kSlots],
+                                                  (seq / kSlots) & 1));
+            if (!ok) break;
+            base = slots + (seq % kSlots) * kSlotBytes;
+            const int left = req.len - tok;
+            if (left < kStep) {  // rows past the last token: 0 * NaN would stay
+                for (int e = left * 8 + lane; e < kStep * 8; e += 32)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+                        asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};" ::"r"(
+                                         base + h * (kStep * 128) + e * 16),
+                                     "r"(0)
+                                     : "memory");
+                __syncwarp();
+            }
+#pragma unroll
+            for (int d = 0; d < 8; ++d) {  // 16 dimensions: matrices (tokens 0-7 | 8-15) x (d | d + 8)
+                uint32_t a[4];
+                const int row = (lane & 7) + ((lane >> 4) << 3), j = 2 * d + ((lane >> 3) & 1);
+                ldsm4t(base + (j >> 3) * (kStep * 128) + row * 128 + (((j & 7) ^ (row & 7)) << 4), a);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    float t[4] = {0.f, 0.f, 0.f, 0.f};
+                    mma<BF>(t, a, pf[n][0], pf[n][1]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[n][d][e] += t[e];
+                }
+            }
+            __syncwarp();
+            ++seq;
+            send();
+        }
+        // (after a wait that has run out the CTA goes on to the end of this part, whose result is void)
+        // ---- the warps meet: (maximum, sum), then O in each warp's own ring ----
+        float* mine_o = reinterpret_cast<float*>(ring_ptr + warp * kSlots * kSlotBytes);
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                float x = l[n][e];
+                x += __shfl_xor_sync(0xffffffffu, x, 4);
+                x += __shfl_xor_sync(0xffffffffu, x, 8);
+                x += __shfl_xor_sync(0xffffffffu, x, 16);
+                const int row = 8 * n + 2 * c + e;
+                if (r8 == 0) s->wml[warp][row] = make_float2(m[n][e], x);
+                if (mine > 0 && row < rows)
+#pragma unroll
+                    for (int d = 0; d < 8; ++d) {
+                        mine_o[row * kRow + 16 * d + r8] = o[n][d][e];
+                        mine_o[row * kRow + 16 * d + 8 + r8] = o[n][d][e + 2];
+                    }
+            }
+        __syncthreads();
+        if (tid < rows) {
+            float M = -INFINITY, sum = 0.f;
+            for (int w = 0; w < kWarps; ++w) M = fmaxf(M, s->wml[w][tid].x);
+            for (int w = 0; w < kWarps; ++w) {
+                const float2 ml = s->wml[w][tid];
+                const float f = ml.x == -INFINITY && ml.y == 0.f ? 0.f : ex2((ml.x - M) * p.scale_log2);
+                s->weight[w][tid] = f;
+                sum = fmaf(ml.y, f, sum);
+            }
+            s->ml[tid] = make_float2(M, sum);
+        }
+        __syncthreads();
+        const bool whole = u == at && end == at + units;
+        const int64_t slot = 2 * (int64_t)blockIdx.x + (u > at ? 0 : 1);
+        for (int e = tid; e < rows * 32; e += kThreads) {
+            const int row = e >> 5, d = (e & 31) * 4;
+            float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int w = 0; w < kWarps; ++w) {
+                const float f = s->weight[w][row];
+                if (f == 0.f) continue;  // (a warp without tokens wrote nothing)
+                const float4 v = *reinterpret_cast<const float4*>(
+                    reinterpret_cast<const float*>(ring_ptr + w * kSlots * kSlotBytes) +
+                    row * kRow + d);
+                a.x = fmaf(v.x, f, a.x);
+                a.y = fmaf(v.y, f, a.y);
+                a.z = fmaf(v.z, f, a.z);
+                a.w = fmaf(v.w, f, a.w);
+            }
+            if (whole) {
+                const float sum = s->ml[row].y, inv = sum == 0.f ? 0.f : 1.f / sum;
+                *reinterpret_cast<uint2*>(
+                    p.out + ((int64_t)(req.s0 + row / p.G) * p.Hq + g * p.G + row % p.G) * kPagedDim +
+                    d) = make_uint2(H::pack(a.x * inv, a.y * inv), H::pack(a.z * inv, a.w * inv));
+            } else {
+                __stcg(reinterpret_cast<float4*>(p.part + (slot * p.part_rows + row) * kPagedDim + d), a);
+            }
+        }
+        if (!whole) {
+            if (tid < rows) __stcg(&p.ml[slot * p.part_rows + tid], s->ml[tid]);
+            const int first = cta_of(at, s->W, s->ctas), last = cta_of(at + units - 1, s->W, s->ctas);
+            __threadfence();
+            __syncthreads();
+            if (tid == 0) {
+                const uint32_t n = atomicAdd(&p.count[first], 1u);
+                s->last = n == (uint32_t)(last - first);
+                if (s->last) p.count[first] = 0;
+                __threadfence();
+            }
+            __syncthreads();
+            if (s->last)
+                for (int e = tid; e < rows * 32; e += kThreads) {
+                    const int row = e >> 5, d = (e & 31) * 4;
+                    float M = -INFINITY, sum = 0.f;
+                    auto at_part = [&](int k) {
+                        return (2 * (int64_t)(first + k) + (k == 0 ? 1 : 0)) * p.part_rows + row;
+                    };
+#pragma unroll 8
+                    for (int k = 0; k <= last - first; ++k) M = fmaxf(M, __ldcg(&p.ml[at_part(k)]).x);
+                    float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+                    for (int k = 0; k <= last - first; ++k) {
+                        const float2 ml = __ldcg(&p.ml[at_part(k)]);
+                        const float4 v = __ldcg(
+                            reinterpret_cast<const float4*>(p.part + at_part(k) * kPagedDim + d));
+                        const float f =
+                            ml.x == -INFINITY && ml.y == 0.f ? 0.f : ex2((ml.x - M) * p.scale_log2);
+                        sum = fmaf(ml.y, f, sum);
+                        a.x = fmaf(v.x, f, a.x);
+                        a.y = fmaf(v.y, f, a.y);
+                        a.z = fmaf(v.z, f, a.z);
+                        a.w = fmaf(v.w, f, a.w);
+                    }
+                    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+                    *reinterpret_cast<uint2*>(
+                        p.out +
+                        ((int64_t)(req.s0 + row / p.G) * p.Hq + g * p.G + row % p.G) * kPagedDim + d) =
+                        make_uint2(H::pack(a.x * inv, a.y * inv), H::pack(a.z * inv, a.w * inv));
+                }
+        }
+        // the rings are free again (their plain accesses before the next copies)
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncthreads();
+        if (*(volatile uint32_t*)&s->abort) break;
+        u = end;
+        if (u == at + units) {
+            at += units;
+            if (++g == p.kv.Hkv) {
+                g = 0;
+                do {
+                    if (++b >= p.kv.batch) break;
+                    req.load(p, b);
+                } while (req.n == 0);
+                if (b >= p.kv.batch) break;
+            }
+        }
+    }
+    // (only after a wait that ran out are copies still in flight)
+    for (uint32_t k = seq; k < issued; ++k)
+        drain(&s->full[warp][k % kSlots], (k / kSlots) & 1);
+    if (tid == 0 && *(volatile uint32_t*)&s->abort) atomicExch(p.status, (uint32_t)LAQ_ERR_TIMEOUT);
+}
+
+}  // namespace
+
+size_t decode_workspace_bytes(int64_t max_q, int G) {
+    const size_t rows = (size_t)kMaxParts * 2 * (max_q * G);
+    return kPartHeader + rows * (kPagedDim * sizeof(float) + sizeof(float2));
+}
+
+laq_status launch_decode(const PagedKv& kv, bool bf, const void* q, int64_t q_stride, int T,
+                         int max_q, int Hq, float scale, void* out, void* workspace,
+                         cudaStream_t stream) {
+    static std::atomic<int> sms_of[kMaxDevices];
+    void (*const kernels[4])(const DecodeParams) = {
+        paged_decode_kernel<false, 1>, paged_decode_kernel<false, 2>, paged_decode_kernel<true, 1>,
+        paged_decode_kernel<true, 2>};
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return LAQ_ERR_CUDA;
+    int sms = sms_of[dev].load();
+    if (sms == 0) {
+        if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
+            return LAQ_ERR_CUDA;
+        for (auto k : kernels)
+            if (cudaFuncSetAttribute((const void*)k, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                     kSmem) != cudaSuccess)
+                return LAQ_ERR_CUDA;
+        if (sms > kPartCtas) sms = kPartCtas;
+        sms_of[dev].store(sms);
+    }
+    DecodeParams p = {};
+    p.kv = kv;
+    p.q = static_cast<const uint16_t*>(q);
+    p.out = static_cast<uint16_t*>(out);
+    p.q_stride = q_stride;
+    p.G = Hq / kv.Hkv;
+    p.Hq = Hq;
+    p.T = T;
+    p.max_q = max_q;
+    p.part_rows = max_q * p.G;
+    p.scale_log2 = scale * 1.44269504088896340736f;
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
+    p.status = reinterpret_cast<uint32_t*>(ws);
+    p.count = p.status + kCountAt;
+    p.part = reinterpret_cast<float*>(ws + kPartHeader);
+    p.ml = reinterpret_cast<float2*>(p.part + (size_t)kMaxParts * 2 * p.part_rows * kPagedDim);
+    const int P = 1 << kv.page_bits, box = P < kStep ? P : kStep;
+    if (!encode_cache(&p.kmap, kv, bf, kv.k, box) || !encode_cache(&p.vmap, kv, bf, kv.v, box))
+        return LAQ_ERR_CUDA;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(2 * sms));
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = kSmem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernels[(bf ? 2 : 0) + (p.part_rows > 8 ? 1 : 0)], p) ==
+                   cudaSuccess
+               ? LAQ_OK
+               : LAQ_ERR_CUDA;
+}
+
+}  // namespace laq
