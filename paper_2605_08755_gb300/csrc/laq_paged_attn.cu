@@ -37,13 +37,27 @@ constexpr int kTile = 128;              // tokens of a K / V tile, rows of a q t
 constexpr int kHalf = kTile * 128;      // bytes of 64 columns of a tile: rows of 128 bytes
 constexpr int kTileBytes = 2 * kHalf;
 constexpr int kStages = 5;              // K and V tiles in flight (160 KB)
-constexpr int kThreads = 320;           // 2 warpgroups of softmax, a TMA warp, an MMA warp
+// Two warpgroups of softmax, and one of a TMA warp, an MMA warp, a warp that walks the items and one more: a
+// softmax thread has a row of 128 scores in registers, and what it would spill goes to L2 (shared
+// memory leaves no L1), so the third warpgroup's registers move to the first two.
+constexpr int kThreads = 384;
+constexpr int kRegsSoft = 200, kRegsRest = 104;  // 2 * 200 + 104 = 3 * 168, the launch's registers
+constexpr int kQueue = 4;
 constexpr int kSmemTiles = (2 + kStages) * kTileBytes;
 constexpr float kGrow = 8.f;            // how far a maximum may grow before O is rescaled (log2)
 
+// The part of an item that one CTA works on: tiles lo .. hi - 1 of its nt (0: no row of it sees a token;
+// -1: the end of the CTA's share).
+struct Piece {
+    int nt, lo, hi, b, g, row0, ntok, pos0, len;
+    int narrow;                      // one q tile
+    int split, slot, parts, index, first;  // of `parts` parts, the one `index`, of CTAs first ..
+};
+
 struct Bars {
     uint64_t full[kStages], empty[kStages], q_full, q_empty, v_tail, drain;
-    uint64_t s_full[2], p_full[2], o_full[2], soft;
+    uint64_t s_full[2], p_full[2], o_full[2], soft, work_full[kQueue], work_empty[kQueue];
+    Piece queue[kQueue], pend[2];       // pieces in work; split ones that wait for their other parts
     uint32_t tmem, abort;
     int b, g, t, off;                   // where this CTA's share starts
     long long left, U, W;
@@ -123,11 +137,47 @@ __device__ __forceinline__ void tm_st32(uint32_t a, const uint32_t* u) {
         "r"(u[30]), "r"(u[31]), "r"(a)
         : "memory");
 }
+// 8 columns
+__device__ __forceinline__ void tm_ld8(uint32_t a, float* r) {
+    uint32_t* u = reinterpret_cast<uint32_t*>(r);
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]),
+                   "=r"(u[6]), "=r"(u[7])
+                 : "r"(a));
+}
+__device__ __forceinline__ void tm_st8(uint32_t a, const float* r) {
+    const uint32_t* u = reinterpret_cast<const uint32_t*>(r);
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0,%1,%2,%3,%4,%5,%6,%7};" ::"r"(u[0]),
+                 "r"(u[1]), "r"(u[2]), "r"(u[3]), "r"(u[4]), "r"(u[5]), "r"(u[6]), "r"(u[7]), "r"(a)
+                 : "memory");
+}
+__device__ __forceinline__ void pin8(float* r) {
+    asm volatile("" : "+f"(r[0]), "+f"(r[1]), "+f"(r[2]), "+f"(r[3]), "+f"(r[4]), "+f"(r[5]),
+                 "+f"(r[6]), "+f"(r[7]));
+}
 __device__ __forceinline__ void tm_wait_ld() {
     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 }
 __device__ __forceinline__ void tm_wait_st() {
     asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+}
+// two fp32 operations an instruction
+__device__ __forceinline__ void fma2(float& x, float& y, float a, float b) {  // (x, y) * a + b
+    asm("{\n.reg .b64 u, v, w;\nmov.b64 u, {%0, %1};\nmov.b64 v, {%2, %2};\nmov.b64 w, {%3, %3};\n"
+        "fma.rn.f32x2 u, u, v, w;\nmov.b64 {%0, %1}, u;\n}\n"
+        : "+f"(x), "+f"(y)
+        : "f"(a), "f"(b));
+}
+__device__ __forceinline__ void add2(float& x, float& y, float a, float b) {
+    asm("{\n.reg .b64 u, v;\nmov.b64 u, {%0, %1};\nmov.b64 v, {%2, %3};\n"
+        "add.rn.f32x2 u, u, v;\nmov.b64 {%0, %1}, u;\n}\n"
+        : "+f"(x), "+f"(y)
+        : "f"(a), "f"(b));
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
 }
 // Pins loaded values behind the wait that makes them valid.
 __device__ __forceinline__ void pin32(float* r) {
@@ -185,60 +235,6 @@ struct Req {
     // units of all items of one kv head
     __device__ long long units(const ChunkParams& p) const {
         return m == 0 ? 0 : m + tiles_before(p, m - 1) + tiles(p, m - 1);
-    }
-};
-
-// The part of an item that one CTA works on: tiles lo .. hi - 1 of nt.
-struct Piece {
-    int b, g, row0, ntok, pos0, len, nt, lo, hi;
-    long long U;  // the item's first unit
-    __device__ bool whole() const { return lo == 0 && hi == nt; }
-};
-
-struct Walk {
-    const ChunkParams& p;
-    long long left, U;
-    int b, g, t, off;
-    Req r;
-    __device__ Walk(const ChunkParams& p_, const Bars* s)
-        : p(p_), left(s->left), U(s->U), b(s->b), g(s->g), t(s->t), off(s->off) {
-        if (left > 0) r.load(p, b);
-    }
-    __device__ bool next(Piece& x) {
-        while (left > 0) {
-            const int nt = r.tiles(p, t), units = nt + 1;
-            const int take = (int)min(left, (long long)(units - off));
-            x.b = b;
-            x.g = g;
-            x.row0 = r.s0 + t * 2 * p.tau;
-            x.ntok = min(r.n - t * 2 * p.tau, 2 * p.tau);
-            x.pos0 = r.past + t * 2 * p.tau;
-            x.len = r.len;
-            x.nt = nt;
-            x.lo = max(off - 1, 0);
-            x.hi = off + take - 1;
-            x.U = U;
-            left -= take;
-            if (off + take == units) {
-                off = 0;
-                U += units;
-                if (++t == r.m) {
-                    t = 0;
-                    if (++g == p.kv.Hkv) {
-                        g = 0;
-                        do {
-                            if (++b >= p.kv.batch) {
-                                left = 0;
-                                break;
-                            }
-                            r.load(p, b);
-                        } while (r.m == 0);
-                    }
-                }
-            }
-            if (x.hi > x.lo || x.nt == 0) return true;
-        }
-        return false;
     }
 };
 
@@ -301,17 +297,86 @@ __device__ void plan(const ChunkParams& p, Bars* s) {
 }
 
 // ---- roles ----
+// Walks the CTA's share and puts its pieces into the queue.
+__device__ void walk_role(const ChunkParams& p, Bars* s) {
+    long long left = s->left, U = s->U;
+    int b = s->b, g = s->g, t = s->t, off = s->off;
+    s->pend[0].nt = s->pend[1].nt = 0;
+    Req r;
+    if (left > 0) r.load(p, b);
+    for (uint32_t n = 0;; ++n) {
+        Piece* x = &s->queue[n % kQueue];
+        if (n >= kQueue &&
+            !bar_wait(&s->abort, &s->work_empty[n % kQueue], (n / kQueue - 1) & 1))
+            return;
+        bool found = false;
+        while (left > 0 && !found) {
+            const int nt = r.tiles(p, t), units = nt + 1;
+            const int take = (int)min(left, (long long)(units - off));
+            const int lo = max(off - 1, 0), hi = off + take - 1;
+            found = hi > lo || nt == 0;
+            if (found) {
+                x->nt = nt;
+                x->lo = lo;
+                x->hi = hi;
+                x->b = b;
+                x->g = g;
+                x->row0 = r.s0 + t * 2 * p.tau;
+                x->ntok = min(r.n - t * 2 * p.tau, 2 * p.tau);
+                x->pos0 = r.past + t * 2 * p.tau;
+                x->len = r.len;
+                x->narrow = x->ntok <= p.tau;
+                x->split = nt > 0 && !(lo == 0 && hi == nt);
+                x->slot = lo > 0 ? 0 : 1;
+                x->first = blockIdx.x;
+                x->parts = 1;
+                x->index = 0;
+                if (x->split) {
+                    x->first = cta_of(U + 1, s->W, s->ctas);
+                    x->parts = cta_of(U + nt, s->W, s->ctas) - x->first + 1;
+                    x->index = (int)blockIdx.x - x->first;
+                    s->pend[x->slot] = *x;
+                }
+            }
+            left -= take;
+            if (off + take == units) {
+                off = 0;
+                U += units;
+                if (++t == r.m) {
+                    t = 0;
+                    if (++g == p.kv.Hkv) {
+                        g = 0;
+                        do {
+                            if (++b >= p.kv.batch) {
+                                left = 0;
+                                break;
+                            }
+                            r.load(p, b);
+                        } while (r.m == 0);
+                    }
+                }
+            }
+        }
+        if (!found) x->nt = -1;
+        bar_arrive(&s->work_full[n % kQueue]);
+        if (!found) return;
+    }
+}
+
 template <bool BF>
 __device__ void load_role(const ChunkParams& p, Bars* s, uint32_t smem) {
     const int lane = threadIdx.x & 31;
     const int P = 1 << p.kv.page_bits, box = min(P, kTile);
-    Walk w(p, s);
-    Piece x;
     uint32_t fills = 0, pieces = 0, tails = 0;
     bool ok = true;
-    while (ok && w.next(x)) {
+    for (uint32_t n = 0;; ++n) {
+        if (!warp_wait(s, &s->work_full[n % kQueue], (n / kQueue) & 1)) break;
+        const Piece x = s->queue[n % kQueue];
+        if (x.nt < 0) break;
+        __syncwarp();
+        if (lane == 0) bar_arrive(&s->work_empty[n % kQueue]);
         if (x.nt == 0) continue;
-        const bool narrow = x.ntok <= p.tau;
+        const bool narrow = x.narrow;
         // Q: row = token * G + head, as the box packs them
         if (pieces && !warp_wait(s, &s->q_empty, (pieces - 1) & 1)) break;
         ++pieces;
@@ -379,6 +444,7 @@ __device__ void load_role(const ChunkParams& p, Bars* s, uint32_t smem) {
             pk = pk1;
             pk1 = pk2;
         }
+        if (!ok) break;
     }
     // copies in flight end before the CTA does (only after a wait that ran out are there any)
     if (*(volatile uint32_t*)&s->abort) {
@@ -394,9 +460,7 @@ __device__ void mma_role(const ChunkParams& p, Bars* s, uint32_t smem, uint32_t 
     constexpr uint32_t kFmt = BF ? 1u : 0u;
     constexpr uint32_t kQk = 1u << 4 | kFmt << 7 | kFmt << 10 | (kTile / 8) << 17 | (kTile / 16) << 24;
     constexpr uint32_t kPv = kQk | 1u << 16;  // B (V): N is the contiguous dimension
-    Walk w(p, s);
-    Piece x;
-    uint32_t use = 0, pieces = 0, np[2] = {0, 0};
+    uint32_t use = 0, pieces = 0, np0 = 0, np1 = 0;
     auto stage = [&](uint32_t f) { return smem + (2 + f % kStages) * kTileBytes; };
     auto wait_full = [&](uint32_t f) {
         return bar_wait(&s->abort, &s->full[f % kStages], (f / kStages) & 1);
@@ -417,14 +481,19 @@ __device__ void mma_role(const ChunkParams& p, Bars* s, uint32_t smem, uint32_t 
             mma_ts(tmem + 256 + 128 * i, tmem + 128 * i + 8 * kk, vdesc(v + kk * 2048), kPv,
                    kk > 0 || !first);
     };
-    auto wait_p = [&](int i) { return bar_wait(&s->abort, &s->p_full[i], np[i]++ & 1); };
+    auto wait_p = [&](int i) {
+        return bar_wait(&s->abort, &s->p_full[i], (i ? np1++ : np0++) & 1);
+    };
     bool ok = true;
-    while (ok && w.next(x)) {
-        if (x.nt == 0) continue;
-        const bool narrow = x.ntok <= p.tau;
+    for (uint32_t w = 0; ok; ++w) {
+        if (!bar_wait(&s->abort, &s->work_full[w % kQueue], (w / kQueue) & 1)) break;
+        const int nt = s->queue[w % kQueue].nt, n = s->queue[w % kQueue].hi - s->queue[w % kQueue].lo;
+        const bool narrow = s->queue[w % kQueue].narrow;
+        if (nt < 0) break;
+        bar_arrive(&s->work_empty[w % kQueue]);
+        if (nt == 0) continue;
         if (!bar_wait(&s->abort, &s->q_full, pieces & 1)) break;
         ++pieces;
-        const int n = x.hi - x.lo;
         if (!narrow) {
             uint32_t kf = use;  // fill of K_j; V_j is the next
             if (!(ok = wait_full(kf))) break;
@@ -487,10 +556,6 @@ __device__ void mma_role(const ChunkParams& p, Bars* s, uint32_t smem, uint32_t 
     }
 }
 
-struct Pending {  // a split piece whose rows wait for the other parts
-    int on, slot, parts, index, first, row0, rows, g, narrow;
-};
-
 template <bool BF>
 __device__ void store_row(const ChunkParams& p, int64_t row, int head, const float (&o)[32], int c0,
                           float f) {
@@ -508,7 +573,7 @@ __device__ void store_row(const ChunkParams& p, int64_t row, int head, const flo
 // Add the parts of `rows` rows from r0: part k in slot (k == 0 ? 1 : 0) of CTA first + k, for narrow
 // items as two halves of rows.  A float4 of a row per thread.
 template <bool BF>
-__device__ void add_parts(const ChunkParams& p, const Pending& d, int r0, int r1) {
+__device__ void add_parts(const ChunkParams& p, const Piece& d, int r0, int r1) {
     const int sources = d.narrow ? 2 * d.parts : d.parts;
     auto base = [&](int k) {
         const int part = d.narrow ? k >> 1 : k;
@@ -548,37 +613,27 @@ __device__ void add_parts(const ChunkParams& p, const Pending& d, int r0, int r1
 
 template <bool BF>
 __device__ void softmax_role(const ChunkParams& p, Bars* s, uint32_t tmem) {
-    const int wg = threadIdx.x >> 7, r = threadIdx.x & 127, warp = threadIdx.x >> 5;
-    const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // the warp's 32 lanes of tensor memory
+    const int wg = threadIdx.x >> 7, r = threadIdx.x & 127;
+    const uint32_t lanes = (uint32_t)((threadIdx.x >> 5) & 3) << 21;  // the warp's lanes of tensor memory
     const uint32_t ts = tmem + lanes + 128 * wg, to = tmem + lanes + 256 + 128 * wg;
     const float c = p.scale_log2, offset = BF ? 0.f : 7.f;
-    Walk w(p, s);
-    Piece x;
-    Pending pend[2] = {};
     uint32_t ns = 0, no = 0, met = 0;
     bool ok = true;
-    while (ok && w.next(x)) {
-        const bool narrow = x.ntok <= p.tau;
-        const int rows = x.ntok * p.G, per = p.tau * p.G;
+    for (uint32_t w = 0; ok; ++w) {
+        if (!(ok = warp_wait(s, &s->work_full[w % kQueue], (w / kQueue) & 1))) break;
+        const Piece& x = s->queue[w % kQueue];
+        if (x.nt < 0) break;
+        const bool narrow = x.narrow;
+        const int per = p.tau * p.G;
         const int r_item = narrow ? r : wg * per + r;  // row of the item
-        const bool valid = r < per && r_item < rows;
-        const int64_t orow = x.row0 + r_item / p.G;
-        const int ohead = x.g * p.G + r_item % p.G;
-        if (x.nt == 0) {  // no row of the item sees a token
-            if (valid && !(narrow && wg)) {
-                float z[32];
-#pragma unroll
-                for (int e = 0; e < 32; ++e) z[e] = 0.f;
-                for (int q = 0; q < 4; ++q) store_row<BF>(p, orow, ohead, z, 32 * q, 0.f);
-            }
-            continue;
-        }
+        const bool valid = r < per && r_item < x.ntok * p.G;
+        const bool busy = __any_sync(0xffffffffu, valid);  // (other warps only keep the order)
         const int seen = x.pos0 + (valid ? r_item / p.G : 0) + 1;     // tokens this row sees
         const int least = x.pos0 + (narrow ? 0 : wg * p.tau) + 1;    // .. the tile's first row sees
-        const bool busy = __any_sync(0xffffffffu, valid);  // (other warps only keep the order)
+        const int hi = x.hi, step = narrow ? 2 : 1;
         float m = -INFINITY, l = 0.f;
         bool first = true;
-        for (int j = x.lo + (narrow ? wg : 0); j < x.hi; j += narrow ? 2 : 1) {
+        for (int j = x.lo + (narrow ? wg : 0); j < hi; j += step) {
             if (!(ok = warp_wait(s, &s->s_full[wg], ns++ & 1))) break;
             tc_after();
             if (!busy) {
@@ -601,28 +656,26 @@ __device__ void softmax_role(const ChunkParams& p, Bars* s, uint32_t tmem) {
             }
             float mx[4] = {v[0], v[1], v[2], v[3]};
 #pragma unroll
-            for (int e = 4; e < 128; ++e) mx[e & 3] = fmaxf(mx[e & 3], v[e]);
-            const float mn = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+            for (int e = 4; e < 124; e += 2) mx[(e >> 1) & 3] = max3(mx[(e >> 1) & 3], v[e], v[e + 1]);
+            const float mn = max3(max3(mx[0], mx[1], v[124]), max3(mx[2], mx[3], v[125]),
+                                  fmaxf(v[126], v[127]));
             if (first) {
                 m = mn;
                 first = false;
-            } else {
+            } else if (__any_sync(0xffffffffu, valid && (mn - m) * c > kGrow)) {
                 // (the product that last changed O is complete: S came after it)
-                const bool grow = valid && (mn - m) * c > kGrow;
-                if (__any_sync(0xffffffffu, grow)) {
-                    const float to_m = fmaxf(m, mn);
-                    const float f = to_m == -INFINITY ? 1.f : ex2((m - to_m) * c);
-                    m = to_m;
-                    l *= f;
-                    for (int q = 0; q < 4; ++q) {
-                        float o[32];
-                        tm_ld32(to + 32 * q, o);
-                        tm_wait_ld();
-                        pin32(o);
+                const float to_m = fmaxf(m, mn);
+                const float f = to_m == -INFINITY ? 1.f : ex2((m - to_m) * c);
+                m = to_m;
+                l *= f;
+                for (int q = 0; q < 16; ++q) {
+                    float o[8];
+                    tm_ld8(to + 8 * q, o);
+                    tm_wait_ld();
+                    pin8(o);
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) o[e] *= f;
-                        tm_st32(to + 32 * q, reinterpret_cast<const uint32_t*>(o));
-                    }
+                    for (int e = 0; e < 8; ++e) o[e] *= f;
+                    tm_st8(to + 8 * q, o);
                 }
             }
             const float base = (m == -INFINITY ? 0.f : m * c) - offset;
@@ -630,11 +683,13 @@ __device__ void softmax_role(const ChunkParams& p, Bars* s, uint32_t tmem) {
             uint32_t pk[64];
 #pragma unroll
             for (int e = 0; e < 128; e += 2) {
-                const float a = ex2(fmaf(v[e], c, -base)), b = ex2(fmaf(v[e + 1], c, -base));
-                sum[(e >> 1) & 3] += a + b;
-                pk[e >> 1] = Half16<BF>::pack(a, b);
+                fma2(v[e], v[e + 1], c, -base);
+                v[e] = ex2(v[e]);
+                v[e + 1] = ex2(v[e + 1]);
+                add2(sum[e & 2], sum[(e & 2) + 1], v[e], v[e + 1]);
+                pk[e >> 1] = Half16<BF>::pack(v[e], v[e + 1]);
+                if (e == 62) tm_st32(ts, pk);
             }
-            tm_st32(ts, pk);
             tm_st32(ts + 32, pk + 32);
             tm_wait_st();
             tc_before();
@@ -643,51 +698,61 @@ __device__ void softmax_role(const ChunkParams& p, Bars* s, uint32_t tmem) {
             l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
         }
         if (!ok) break;
-        const bool direct = !narrow && x.whole();
-        const int slot = x.lo > 0 ? 0 : 1;
-        const int64_t part = (2 * (int64_t)blockIdx.x + slot) * 2 * p.part_rows + wg * p.part_rows + r;
-        if (!first) {
-            if (!(ok = warp_wait(s, &s->o_full[wg], no++ & 1))) break;
-            tc_after();
-            const float inv = l == 0.f ? 0.f : 1.f / l;
-            for (int q = 0; busy && q < 4; ++q) {
-                float o[32];
-                tm_ld32(to + 32 * q, o);
-                tm_wait_ld();
-                pin32(o);
-                if (valid && direct) {
-                    store_row<BF>(p, orow, ohead, o, 32 * q, inv);
-                } else if (valid) {
-                    float4* dst = reinterpret_cast<float4*>(p.part + part * kPagedDim + 32 * q);
+        const int64_t orow = x.row0 + r_item / p.G;
+        const int ohead = x.g * p.G + r_item % p.G;
+        const bool direct = !narrow && !x.split;
+        if (x.nt == 0) {  // no row of the item sees a token
+            if (valid && !(narrow && wg)) {
+                float z[32];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        __stcg(dst + e, make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2],
-                                                    o[4 * e + 3]));
-                }
-                __syncwarp();
+                for (int e = 0; e < 32; ++e) z[e] = 0.f;
+                for (int q = 0; q < 4; ++q) store_row<BF>(p, orow, ohead, z, 32 * q, 0.f);
             }
-            tc_before();  // (the next item's first product comes after the next P)
-        }
-        if (direct) continue;
-        if (valid) __stcg(&p.ml[part], make_float2(m, l));
-        Pending d;
-        const int cf = cta_of(x.U + 1, s->W, s->ctas), cl = cta_of(x.U + x.nt, s->W, s->ctas);
-        d = Pending{1, slot, cl - cf + 1, (int)blockIdx.x - cf, cf, x.row0, rows, x.g, narrow};
-        if (d.parts == 1) {  // a narrow item of this CTA alone
-            if (!(ok = meet(s, met))) break;
-            add_parts<BF>(p, d, 0, rows);
-            if (!(ok = meet(s, met))) break;
         } else {
-            __threadfence();
-            if (!(ok = meet(s, met))) break;
-            if (threadIdx.x == 0) atomicAdd(&p.count[cf], 1u);
-            pend[slot] = d;
+            const int64_t part =
+                (2 * (int64_t)blockIdx.x + x.slot) * 2 * p.part_rows + wg * p.part_rows + r;
+            if (!first) {
+                if (!(ok = warp_wait(s, &s->o_full[wg], no++ & 1))) break;
+                tc_after();
+                const float inv = l == 0.f ? 0.f : 1.f / l;
+                for (int q = 0; busy && q < 4; ++q) {
+                    float o[32];
+                    tm_ld32(to + 32 * q, o);
+                    tm_wait_ld();
+                    pin32(o);
+                    if (valid && direct) {
+                        store_row<BF>(p, orow, ohead, o, 32 * q, inv);
+                    } else if (valid) {
+                        float4* dst = reinterpret_cast<float4*>(p.part + part * kPagedDim + 32 * q);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            __stcg(dst + e, make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2],
+                                                        o[4 * e + 3]));
+                    }
+                    __syncwarp();
+                }
+                tc_before();  // (the next item's first product comes after the next P)
+            }
+            if (!direct) {
+                if (valid) __stcg(&p.ml[part], make_float2(m, l));
+                if (x.split) {  // the others' parts are looked for at the end of the share
+                    __threadfence();
+                    if (!(ok = meet(s, met))) break;
+                    if (threadIdx.x == 0) atomicAdd(&p.count[x.first], 1u);
+                } else {        // a narrow item of this CTA alone
+                    if (!(ok = meet(s, met))) break;
+                    add_parts<BF>(p, x, 0, x.ntok * p.G);
+                    if (!(ok = meet(s, met))) break;
+                }
+            }
         }
+        __syncwarp();
+        if ((threadIdx.x & 31) == 0) bar_arrive(&s->work_empty[w % kQueue]);
     }
     // the split pieces, once all their parts are there
     for (int k = 0; ok && k < 2; ++k) {
-        const Pending d = pend[k];
-        if (!d.on) continue;
+        const Piece& d = s->pend[k];
+        if (d.nt == 0) continue;
         if (threadIdx.x == 0) {
             uint32_t n = 0;
             const long long t0 = clock64();
@@ -703,8 +768,8 @@ __device__ void softmax_role(const ChunkParams& p, Bars* s, uint32_t tmem) {
         }
         if (!(ok = meet(s, met)) || *(volatile uint32_t*)&s->abort) break;
         __threadfence();
-        add_parts<BF>(p, d, (int)((long long)d.rows * d.index / d.parts),
-                      (int)((long long)d.rows * (d.index + 1) / d.parts));
+        const long long rows = d.ntok * p.G;
+        add_parts<BF>(p, d, (int)(rows * d.index / d.parts), (int)(rows * (d.index + 1) / d.parts));
         if (threadIdx.x == 0) {  // the last to have seen the count clears it
             if (atomicAdd(&p.done[d.first], 1u) == (uint32_t)d.parts - 1) {
                 p.count[d.first] = 0;
@@ -731,6 +796,10 @@ __global__ void __launch_bounds__(kThreads, 1) paged_chunk_kernel(
         bar_init(&s->v_tail, 1);
         bar_init(&s->drain, 1);
         bar_init(&s->soft, 8);
+        for (int i = 0; i < kQueue; ++i) {
+            bar_init(&s->work_full[i], 1);
+            bar_init(&s->work_empty[i], 10);  // 8 softmax warps, the TMA warp, the MMA thread
+        }
         for (int i = 0; i < 2; ++i) {
             bar_init(&s->s_full[i], 1);
             bar_init(&s->p_full[i], 4);
@@ -751,11 +820,13 @@ __global__ void __launch_bounds__(kThreads, 1) paged_chunk_kernel(
     tc_after();
     const uint32_t tmem = s->tmem;
     if (warp < 8) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoft));
         softmax_role<BF>(p, s, tmem);
-    } else if (warp == 8) {
-        load_role<BF>(p, s, smem);
-    } else if ((threadIdx.x & 31) == 0) {
-        mma_role<BF>(p, s, smem, tmem);
+    } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsRest));
+        if (warp == 8) load_role<BF>(p, s, smem);
+        else if (threadIdx.x == 9 * 32) mma_role<BF>(p, s, smem, tmem);
+        else if (threadIdx.x == 10 * 32) walk_role(p, s);
     }
     __syncwarp();
     tc_before();
