@@ -570,44 +570,89 @@ __device__ void store_row(const ChunkParams& p, int64_t row, int head, const flo
     }
 }
 
-// Add the parts of `rows` rows from r0: part k in slot (k == 0 ? 1 : 0) of CTA first + k, for narrow
-// items as two halves of rows.  A float4 of a row per thread.
+// Add the parts of rows r0 .. r1 - 1 of an item: part k is in slot (k == 0 ? 1 : 0) of CTA first + k, a
+// narrow item's as two halves of rows (the two warpgroups').  A warp takes four rows at a time, lane k
+// the weight of source k, every lane four dimensions of the sum.
 template <bool BF>
 __device__ void add_parts(const ChunkParams& p, const Piece& d, int r0, int r1) {
-    const int sources = d.narrow ? 2 * d.parts : d.parts;
-    auto base = [&](int k) {
-        const int part = d.narrow ? k >> 1 : k;
-        const int64_t slot = 2 * (int64_t)(d.first + part) + (part == 0 ? 1 : 0);
-        return slot * 2 * p.part_rows + (d.narrow && (k & 1) ? p.part_rows : 0);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int narrow = d.narrow, sources = narrow ? 2 * d.parts : d.parts, per = p.tau * p.G;
+    auto base = [&](int k) {  // first row of source k
+        const int part = narrow ? k >> 1 : k;
+        return (2 * (d.first + part) + (part == 0 ? 1 : 0)) * 2 * p.part_rows +
+               (narrow && (k & 1) ? p.part_rows : 0);
     };
-    auto row_in = [&](int r) {  // row r of the item: its place in a part
-        const int per = p.tau * p.G;
-        return d.narrow || r < per ? r : p.part_rows + r - per;
-    };
-    for (int e = threadIdx.x; e < (r1 - r0) * 32; e += 256) {
-        const int r = r0 + (e >> 5), c = e & 31, ri = row_in(r);
-        float M = -INFINITY;
-        for (int k = 0; k < sources; ++k) M = fmaxf(M, __ldcg(&p.ml[base(k) + ri]).x);
-        float l = 0.f;
-        float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int k = 0; k < sources; ++k) {
-            const float2 ml = __ldcg(&p.ml[base(k) + ri]);
-            if (ml.x == -INFINITY && ml.y == 0.f) continue;
-            const float f = ex2((ml.x - M) * p.scale_log2);
-            const float4 o =
-                __ldcg(reinterpret_cast<const float4*>(p.part + (base(k) + ri) * kPagedDim) + c);
-            l = fmaf(ml.y, f, l);
-            a.x = fmaf(o.x, f, a.x);
-            a.y = fmaf(o.y, f, a.y);
-            a.z = fmaf(o.z, f, a.z);
-            a.w = fmaf(o.w, f, a.w);
+    for (int rr = r0 + 4 * warp; rr < r1; rr += 32) {
+        int ri[4];  // the rows' places in a part
+        float M[4], l[4];
+        float4 acc[4];
+#pragma unroll
+        for (int a = 0; a < 4; ++a) {
+            const int r = min(rr + a, r1 - 1);
+            ri[a] = narrow || r < per ? r : p.part_rows + r - per;
+            M[a] = -INFINITY;
+            l[a] = 0.f;
+            acc[a] = make_float4(0.f, 0.f, 0.f, 0.f);
         }
-        const float inv = l == 0.f ? 0.f : 1.f / l;
-        const int64_t row = d.row0 + r / p.G;
-        const int head = d.g * p.G + r % p.G;
-        *reinterpret_cast<uint2*>(p.out + (row * p.Hq + head) * kPagedDim + 4 * c) =
-            make_uint2(Half16<BF>::pack(a.x * inv, a.y * inv),
-                       Half16<BF>::pack(a.z * inv, a.w * inv));
+        // (two passes over the maxima where there are more than 32 sources)
+        for (int k0 = 0; sources > 32 && k0 < sources; k0 += 32)
+#pragma unroll
+            for (int a = 0; a < 4; ++a)
+                if (k0 + lane < sources)
+                    M[a] = fmaxf(M[a], __ldcg(&p.ml[base(k0 + lane) + ri[a]]).x);
+        for (int k0 = 0; k0 < sources; k0 += 32) {
+            float w[4];
+            float2 ml[4];
+#pragma unroll
+            for (int a = 0; a < 4; ++a) {
+                ml[a] = make_float2(-INFINITY, 0.f);
+                if (k0 + lane < sources) ml[a] = __ldcg(&p.ml[base(k0 + lane) + ri[a]]);
+            }
+#pragma unroll
+            for (int a = 0; a < 4; ++a) {
+                if (k0 == 0) {
+                    M[a] = fmaxf(M[a], ml[a].x);
+#pragma unroll
+                    for (int o = 16; o > 0; o >>= 1)
+                        M[a] = fmaxf(M[a], __shfl_xor_sync(0xffffffffu, M[a], o));
+                }
+                // (no weight: nothing was written)
+                w[a] = ml[a].x == -INFINITY && ml[a].y == 0.f ? 0.f
+                                                              : ex2((ml[a].x - M[a]) * p.scale_log2);
+                float s = w[a] * ml[a].y;
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+                l[a] += s;
+            }
+            const int n = min(32, sources - k0);
+#pragma unroll 2
+            for (int k = 0; k < n; ++k) {
+                float4 o[4];
+#pragma unroll
+                for (int a = 0; a < 4; ++a)
+                    o[a] = __ldcg(reinterpret_cast<const float4*>(
+                                      p.part + (int64_t)(base(k0 + k) + ri[a]) * kPagedDim) + lane);
+#pragma unroll
+                for (int a = 0; a < 4; ++a) {
+                    const float f = __shfl_sync(0xffffffffu, w[a], k);
+                    if (f == 0.f) continue;
+                    acc[a].x = fmaf(o[a].x, f, acc[a].x);
+                    acc[a].y = fmaf(o[a].y, f, acc[a].y);
+                    acc[a].z = fmaf(o[a].z, f, acc[a].z);
+                    acc[a].w = fmaf(o[a].w, f, acc[a].w);
+                }
+            }
+        }
+#pragma unroll
+        for (int a = 0; a < 4; ++a) {
+            const int r = rr + a;
+            if (r >= r1) break;
+            const float inv = l[a] == 0.f ? 0.f : 1.f / l[a];
+            *reinterpret_cast<uint2*>(
+                p.out + ((int64_t)(d.row0 + r / p.G) * p.Hq + d.g * p.G + r % p.G) * kPagedDim +
+                4 * lane) = make_uint2(Half16<BF>::pack(acc[a].x * inv, acc[a].y * inv),
+                                       Half16<BF>::pack(acc[a].z * inv, acc[a].w * inv));
+        }
     }
 }
 
@@ -642,54 +687,63 @@ __device__ void softmax_role(const ChunkParams& p, Bars* s, uint32_t tmem) {
                 if ((threadIdx.x & 31) == 0) bar_arrive(&s->p_full[wg]);
                 continue;
             }
-            float v[128];
-#pragma unroll
-            for (int q = 0; q < 4; ++q) tm_ld32(ts + 32 * q, v + 32 * q);
-            tm_wait_ld();
-#pragma unroll
-            for (int q = 0; q < 4; ++q) pin32(v + 32 * q);
-            if ((j + 1) * kTile > least) {
-                const int lim = seen - j * kTile;
-#pragma unroll
-                for (int e = 0; e < 128; ++e)
-                    if (e >= lim) v[e] = -INFINITY;
-            }
-            float mx[4] = {v[0], v[1], v[2], v[3]};
-#pragma unroll
-            for (int e = 4; e < 124; e += 2) mx[(e >> 1) & 3] = max3(mx[(e >> 1) & 3], v[e], v[e + 1]);
-            const float mn = max3(max3(mx[0], mx[1], v[124]), max3(mx[2], mx[3], v[125]),
-                                  fmaxf(v[126], v[127]));
-            if (first) {
-                m = mn;
-                first = false;
-            } else if (__any_sync(0xffffffffu, valid && (mn - m) * c > kGrow)) {
-                // (the product that last changed O is complete: S came after it)
-                const float to_m = fmaxf(m, mn);
-                const float f = to_m == -INFINITY ? 1.f : ex2((m - to_m) * c);
-                m = to_m;
-                l *= f;
-                for (int q = 0; q < 16; ++q) {
-                    float o[8];
-                    tm_ld8(to + 8 * q, o);
-                    tm_wait_ld();
-                    pin8(o);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) o[e] *= f;
-                    tm_st8(to + 8 * q, o);
-                }
-            }
-            const float base = (m == -INFINITY ? 0.f : m * c) - offset;
-            float sum[4] = {0.f, 0.f, 0.f, 0.f};
+            // The exponentials of a tile take the maximum so far on trust, its own being found beside
+            // them; where it has grown too much (and in the first tile) they are taken again.
+            float sum[4];
             uint32_t pk[64];
+            for (bool trust = !first;; trust = false) {
+                float v[128];
 #pragma unroll
-            for (int e = 0; e < 128; e += 2) {
-                fma2(v[e], v[e + 1], c, -base);
-                v[e] = ex2(v[e]);
-                v[e + 1] = ex2(v[e + 1]);
-                add2(sum[e & 2], sum[(e & 2) + 1], v[e], v[e + 1]);
-                pk[e >> 1] = Half16<BF>::pack(v[e], v[e + 1]);
-                if (e == 62) tm_st32(ts, pk);
+                for (int q = 0; q < 4; ++q) tm_ld32(ts + 32 * q, v + 32 * q);
+                tm_wait_ld();
+#pragma unroll
+                for (int q = 0; q < 4; ++q) pin32(v + 32 * q);
+                if ((j + 1) * kTile > least) {
+                    const int lim = seen - j * kTile;
+#pragma unroll
+                    for (int e = 0; e < 128; ++e)
+                        if (e >= lim) v[e] = -INFINITY;
+                }
+                float mx[4] = {v[0], v[1], v[2], v[3]};
+                if (!trust) {
+#pragma unroll
+                    for (int e = 4; e < 128; e += 2)
+                        mx[(e >> 1) & 3] = max3(mx[(e >> 1) & 3], v[e], v[e + 1]);
+                    const float mn = fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]);
+                    const float to_m = fmaxf(m, mn);
+                    if (!first) {
+                        // (the product that last changed O is complete: S came after it)
+                        const float f = to_m == -INFINITY ? 1.f : ex2((m - to_m) * c);
+                        l *= f;
+                        for (int q = 0; q < 16; ++q) {
+                            float o[8];
+                            tm_ld8(to + 8 * q, o);
+                            tm_wait_ld();
+                            pin8(o);
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) o[e] *= f;
+                            tm_st8(to + 8 * q, o);
+                        }
+                    }
+                    m = to_m;
+                }
+                const float base = (m == -INFINITY ? 0.f : m * c) - offset;
+                sum[0] = sum[1] = sum[2] = sum[3] = 0.f;
+#pragma unroll
+                for (int e = 0; e < 128; e += 2) {
+                    mx[(e >> 1) & 3] = max3(mx[(e >> 1) & 3], v[e], v[e + 1]);
+                    fma2(v[e], v[e + 1], c, -base);
+                    v[e] = ex2(v[e]);
+                    v[e + 1] = ex2(v[e + 1]);
+                    add2(sum[e & 2], sum[(e & 2) + 1], v[e], v[e + 1]);
+                    pk[e >> 1] = Half16<BF>::pack(v[e], v[e + 1]);
+                }
+                if (!trust) break;
+                const float mn = fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]);
+                if (!__any_sync(0xffffffffu, valid && (mn - m) * c > kGrow)) break;
             }
+            first = false;
+            tm_st32(ts, pk);
             tm_st32(ts + 32, pk + 32);
             tm_wait_st();
             tc_before();
