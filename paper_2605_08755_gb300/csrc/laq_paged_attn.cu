@@ -17,7 +17,7 @@
 // shared memory, since 0 * NaN would not vanish in the product.
 //
 // Work split: one CTA per SM walks an equal share of all items' tiles in order (a "unit" is a tile
-// of 128 tokens of an item, and one more unit for each item's start); an item that a share's border
+// of 128 tokens of an item; kStart more units stand for each item's start and end); an item that a share's border
 // cuts is finished by its CTAs together: each writes its part's O, maximum and sum to the workspace,
 // and when all of them are there each adds up a share of the rows, in the order of the parts.
 #include <cuda.h>
@@ -36,14 +36,17 @@ namespace {
 constexpr int kTile = 128;              // tokens of a K / V tile, rows of a q tile
 constexpr int kHalf = kTile * 128;      // bytes of 64 columns of a tile: rows of 128 bytes
 constexpr int kTileBytes = 2 * kHalf;
-constexpr int kStages = 5;              // K and V tiles in flight (160 KB)
+constexpr int kStages = 4;              // K and V tiles in flight (128 KB)
 // Two warpgroups of softmax, and one of a TMA warp, an MMA warp, a warp that walks the items and one more: a
 // softmax thread has a row of 128 scores in registers, and what it would spill goes to L2 (shared
 // memory leaves no L1), so the third warpgroup's registers move to the first two.
 constexpr int kThreads = 384;
-constexpr int kRegsSoft = 200, kRegsRest = 104;  // 2 * 200 + 104 = 3 * 168, the launch's registers
+constexpr int kRegsSoft = 208, kRegsRest = 88;  // 2 * 208 + 88 = 3 * 168, the launch's registers
 constexpr int kQueue = 4;
-constexpr int kSmemTiles = (2 + kStages) * kTileBytes;
+constexpr int kStaging = (2 + kStages) * kTileBytes;  // where: 4 KB for each softmax warp
+constexpr int kSmemTiles = kStaging + 8 * 4096;
+constexpr int kMinUnits = 4;            // fewer are not worth a CTA of their own
+constexpr int kStart = 2;               // what starting and ending an item costs, in tiles
 constexpr float kGrow = 8.f;            // how far a maximum may grow before O is rescaled (log2)
 
 // The part of an item that one CTA works on: tiles lo .. hi - 1 of its nt (0: no row of it sees a token;
@@ -59,9 +62,10 @@ struct Bars {
     uint64_t s_full[2], p_full[2], o_full[2], soft, work_full[kQueue], work_empty[kQueue];
     Piece queue[kQueue], pend[2];       // pieces in work; split ones that wait for their other parts
     uint32_t tmem, abort;
-    int b, g, t, off;                   // where this CTA's share starts
-    long long left, U, W;
-    int ctas;
+    int b;                              // this CTA's share: from unit `into` of request b, which starts at
+    long long into, at, left;           // unit `at`; `left` units
+    Shares shares;
+    float2 ml[kTile];                   // (maximum, sum) of the second warpgroup's rows
     long long scan[kThreads / 32];
 };
 constexpr int kSmem = kSmemTiles + 1024 + (int)sizeof(Bars);
@@ -212,33 +216,39 @@ struct Req {
         return (max(end, 0) + kTile - 1) / kTile;
     }
     // tiles of the first x items (x < m): sum of ceil(max(0, past + (t + 1) 2 tau) / 128), as a sum of
-    // floors of a line, by Euclid's algorithm
+    // floors of a line, by Euclid's algorithm (every term fits 32 bits)
     __device__ long long tiles_before(const ChunkParams& p, int x) const {
-        const int S = 2 * p.tau;
-        const int skip = past < 0 ? min(x, (int)(-(long long)past / S)) : 0;
-        long long sum = 0, n_ = x - skip, M = kTile, a = S,
-                  b = (long long)past + (skip + 1LL) * S + kTile - 1;
-        while (n_ > 0) {
-            sum += n_ * (n_ - 1) / 2 * (a / M) + n_ * (b / M);
-            a %= M;
-            b %= M;
-            const long long y = a * n_ + b;
+        const uint32_t S = 2 * p.tau;
+        const uint32_t skip = past < 0 ? min((uint32_t)x, (uint32_t)(-(long long)past) / S) : 0;
+        long long sum = 0;
+        uint32_t n = x - skip, M = kTile, a = S,
+                 b = (uint32_t)(past + (int)((skip + 1) * S)) + kTile - 1;
+        while (n > 0) {
+            const uint32_t qa = a / M, qb = b / M;
+            sum += (long long)n * (n - 1) / 2 * qa + (long long)n * qb;
+            a -= qa * M;
+            b -= qb * M;
+            const uint32_t y = a * n + b;
             if (y < M) break;
-            n_ = y / M;
-            b = y % M;
-            const long long s = M;
+            n = y / M;
+            b = y - n * M;
+            const uint32_t t = M;
             M = a;
-            a = s;
+            a = t;
         }
         return sum;
     }
+    // the first unit of item t < m
+    __device__ long long start(const ChunkParams& p, int t) const {
+        return (long long)kStart * t + tiles_before(p, t);
+    }
     // units of all items of one kv head
     __device__ long long units(const ChunkParams& p) const {
-        return m == 0 ? 0 : m + tiles_before(p, m - 1) + tiles(p, m - 1);
+        return m == 0 ? 0 : start(p, m - 1) + kStart + tiles(p, m - 1);
     }
 };
 
-// Every thread takes a run of requests; one of them finds where the CTA's share starts.
+// Every thread takes a run of requests; one of them finds the request where the CTA's share starts.
 __device__ void plan(const ChunkParams& p, Bars* s) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int per = (p.kv.batch + kThreads - 1) / kThreads;
@@ -264,46 +274,52 @@ __device__ void plan(const ChunkParams& p, Bars* s) {
         W += s->scan[k];
     }
     before += inc - sum;
-    const int ctas = (int)max(1LL, min((long long)gridDim.x, W / p.min_units));
+    const int ctas = (int)max(1LL, min((long long)gridDim.x, W / kMinUnits));
     if (W == 0 || (int)blockIdx.x >= ctas) return;
-    const long long u0 = W * blockIdx.x / ctas, u1 = W * (blockIdx.x + 1) / ctas;
+    Shares sh;
+    sh.set(W, ctas);
+    const long long u0 = sh.start(blockIdx.x);
     if (u0 < before || u0 >= before + sum) return;
-    long long at = before;
-    int b = b0;
-    for (; b < b1; ++b) {
+    for (int b = b0; b < b1; ++b) {
         r.load(p, b);
         const long long c = r.units(p) * p.kv.Hkv;
-        if (u0 < at + c) break;
-        at += c;
+        if (u0 < before + c) {
+            s->b = b;
+            break;
+        }
+        before += c;
     }
-    const long long per_head = r.units(p);
-    const int g = (int)((u0 - at) / per_head);
-    at += g * per_head;
-    int lo = 0, hi = r.m - 1;  // the last item t with t + tiles_before(t) <= u0 - at
-    while (lo < hi) {
-        const int t = (lo + hi + 1) / 2;
-        if (t + r.tiles_before(p, t) <= u0 - at) lo = t;
-        else hi = t - 1;
-    }
-    at += lo + r.tiles_before(p, lo);
-    s->b = b;
-    s->g = g;
-    s->t = lo;
-    s->off = (int)(u0 - at);
-    s->U = at;
-    s->left = u1 - u0;
-    s->W = W;
-    s->ctas = ctas;
+    s->into = u0 - before;
+    s->at = before;
+    s->left = sh.start(blockIdx.x + 1) - u0;
+    s->shares = sh;
 }
 
 // ---- roles ----
-// Walks the CTA's share and puts its pieces into the queue.
+// Walks the CTA's share and puts its pieces into the queue (a warp: its lanes look for the first item
+// together).
 __device__ void walk_role(const ChunkParams& p, Bars* s) {
-    long long left = s->left, U = s->U;
-    int b = s->b, g = s->g, t = s->t, off = s->off;
-    s->pend[0].nt = s->pend[1].nt = 0;
+    const int lane = threadIdx.x & 31;
+    long long left = s->left, U = 0;
+    int b = s->b, g = 0, t = 0, off = 0;
     Req r;
-    if (left > 0) r.load(p, b);
+    if (left > 0) {
+        r.load(p, b);
+        long long into = s->into;
+        const long long per_head = r.units(p);
+        g = (int)div_ll(into, per_head);
+        into -= g * per_head;
+        for (int n = r.m; n > 1;) {  // the last of items t .. t + n - 1 that starts at or before `into`
+            const int step = (n + 31) / 32, at = (lane + 1) * step;
+            const int c = __popc(__ballot_sync(0xffffffffu, at < n && r.start(p, t + at) <= into));
+            t += c * step;
+            n = min(step, n - c * step);
+        }
+        off = (int)(into - r.start(p, t));
+        U = s->at + g * per_head + into - off;
+    }
+    if (lane != 0) return;
+    s->pend[0].nt = s->pend[1].nt = 0;
     for (uint32_t n = 0;; ++n) {
         Piece* x = &s->queue[n % kQueue];
         if (n >= kQueue &&
@@ -311,10 +327,10 @@ __device__ void walk_role(const ChunkParams& p, Bars* s) {
             return;
         bool found = false;
         while (left > 0 && !found) {
-            const int nt = r.tiles(p, t), units = nt + 1;
+            const int nt = r.tiles(p, t), units = nt + kStart;
             const int take = (int)min(left, (long long)(units - off));
-            const int lo = max(off - 1, 0), hi = off + take - 1;
-            found = hi > lo || nt == 0;
+            const int lo = max(off - kStart, 0), hi = off + take - kStart;
+            found = hi > lo || (nt == 0 && off == 0);
             if (found) {
                 x->nt = nt;
                 x->lo = lo;
@@ -332,8 +348,8 @@ __device__ void walk_role(const ChunkParams& p, Bars* s) {
                 x->parts = 1;
                 x->index = 0;
                 if (x->split) {
-                    x->first = cta_of(U + 1, s->W, s->ctas);
-                    x->parts = cta_of(U + nt, s->W, s->ctas) - x->first + 1;
+                    x->first = s->shares.cta_of(U + kStart);
+                    x->parts = s->shares.cta_of(U + kStart + nt - 1) - x->first + 1;
                     x->index = (int)blockIdx.x - x->first;
                     s->pend[x->slot] = *x;
                 }
@@ -557,24 +573,44 @@ __device__ void mma_role(const ChunkParams& p, Bars* s, uint32_t smem, uint32_t 
 }
 
 template <bool BF>
-__device__ void store_row(const ChunkParams& p, int64_t row, int head, const float (&o)[32], int c0,
-                          float f) {
-    uint16_t* dst = p.out + (row * p.Hq + head) * kPagedDim + c0;
-#pragma unroll
-    for (int c = 0; c < 32; c += 8) {
-        uint32_t u[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            u[e] = Half16<BF>::pack(o[c + 2 * e] * f, o[c + 2 * e + 1] * f);
-        *reinterpret_cast<uint4*>(dst + c) = make_uint4(u[0], u[1], u[2], u[3]);
-    }
+__device__ __forceinline__ uint4 pack8(const float* o, float f) {
+    return make_uint4(Half16<BF>::pack(o[0] * f, o[1] * f), Half16<BF>::pack(o[2] * f, o[3] * f),
+                      Half16<BF>::pack(o[4] * f, o[5] * f), Half16<BF>::pack(o[6] * f, o[7] * f));
 }
 
-// Add the parts of rows r0 .. r1 - 1 of an item: part k is in slot (k == 0 ? 1 : 0) of CTA first + k, a
-// narrow item's as two halves of rows (the two warpgroups').  A warp takes four rows at a time, lane k
-// the weight of source k, every lane four dimensions of the sum.
+// 128 bytes of a row of each lane to the rows' places in memory (null: none), by way of the warp's 4 KB of
+// staging: eight lanes write a row, so that a store covers whole lines (a lane's own row at a time, every
+// store instruction touched 32 of them: 5000 cycles for an item's rows).
+__device__ __forceinline__ void put_rows(uint32_t staging, const uint4 (&c)[8], uint8_t* dst) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(
+                         staging + lane * 128 + ((k ^ (lane & 7)) << 4)),
+                     "r"(c[k].x), "r"(c[k].y), "r"(c[k].z), "r"(c[k].w)
+                     : "memory");
+    __syncwarp();
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        const int row = 4 * k + (lane >> 3);
+        uint4 v;
+        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                     : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+                     : "r"(staging + row * 128 + (((lane & 7) ^ (row & 7)) << 4))
+                     : "memory");
+        uint8_t* to = reinterpret_cast<uint8_t*>(
+            __shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(dst), row));
+        if (to) *reinterpret_cast<uint4*>(to + 16 * (lane & 7)) = v;
+    }
+    __syncwarp();
+}
+
+// Add the parts of rows r0 .. r1 - 1 of a split item: part k is in slot (k == 0 ? 1 : 0) of CTA first + k,
+// a narrow item's as two halves of rows (the two warpgroups').  First the rows' weights, into staging, then
+// a warp takes four rows at a time, a lane four dimensions.
 template <bool BF>
-__device__ void add_parts(const ChunkParams& p, const Piece& d, int r0, int r1) {
+__device__ __noinline__ bool add_parts(const ChunkParams& p, Bars* s, float* staging, uint32_t& met, const Piece& d,
+                          int r0, int r1) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int narrow = d.narrow, sources = narrow ? 2 * d.parts : d.parts, per = p.tau * p.G;
     auto base = [&](int k) {  // first row of source k
@@ -582,82 +618,180 @@ __device__ void add_parts(const ChunkParams& p, const Piece& d, int r0, int r1) 
         return (2 * (d.first + part) + (part == 0 ? 1 : 0)) * 2 * p.part_rows +
                (narrow && (k & 1) ? p.part_rows : 0);
     };
-    for (int rr = r0 + 4 * warp; rr < r1; rr += 32) {
+    auto row_in = [&](int r) { return narrow || r < per ? r : p.part_rows + r - per; };
+    const int rows = r1 - r0;  // (sources * rows fits: at most 2 * (256 + parts) floats)
+    if ((int)threadIdx.x < rows) {
+        const int ri = row_in(r0 + threadIdx.x);
+        float M = -INFINITY, l = 0.f;
+#pragma unroll 8
+        for (int k = 0; k < sources; ++k) M = fmaxf(M, __ldcg(&p.ml[base(k) + ri]).x);
+#pragma unroll 8
+        for (int k = 0; k < sources; ++k) {
+            const float2 ml = __ldcg(&p.ml[base(k) + ri]);
+            // (no weight: nothing was written)
+            const float f =
+                ml.x == -INFINITY && ml.y == 0.f ? 0.f : ex2((ml.x - M) * p.scale_log2);
+            staging[k * rows + threadIdx.x] = f;
+            l = fmaf(f, ml.y, l);
+        }
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        for (int k = 0; k < sources; ++k) staging[k * rows + threadIdx.x] *= inv;
+    }
+    if (!meet(s, met)) return false;
+    for (int rr = 4 * warp; rr < rows; rr += 32) {
         int ri[4];  // the rows' places in a part
-        float M[4], l[4];
         float4 acc[4];
 #pragma unroll
         for (int a = 0; a < 4; ++a) {
-            const int r = min(rr + a, r1 - 1);
-            ri[a] = narrow || r < per ? r : p.part_rows + r - per;
-            M[a] = -INFINITY;
-            l[a] = 0.f;
+            ri[a] = row_in(r0 + min(rr + a, rows - 1));
             acc[a] = make_float4(0.f, 0.f, 0.f, 0.f);
         }
-        // (two passes over the maxima where there are more than 32 sources)
-        for (int k0 = 0; sources > 32 && k0 < sources; k0 += 32)
+#pragma unroll 4
+        for (int k = 0; k < sources; ++k) {
+            float4 o[4];
+            const float4* src = reinterpret_cast<const float4*>(p.part) +
+                                (int64_t)base(k) * (kPagedDim / 4) + lane;
 #pragma unroll
-            for (int a = 0; a < 4; ++a)
-                if (k0 + lane < sources)
-                    M[a] = fmaxf(M[a], __ldcg(&p.ml[base(k0 + lane) + ri[a]]).x);
-        for (int k0 = 0; k0 < sources; k0 += 32) {
-            float w[4];
-            float2 ml[4];
+            for (int a = 0; a < 4; ++a) o[a] = __ldcg(src + ri[a] * (kPagedDim / 4));
 #pragma unroll
             for (int a = 0; a < 4; ++a) {
-                ml[a] = make_float2(-INFINITY, 0.f);
-                if (k0 + lane < sources) ml[a] = __ldcg(&p.ml[base(k0 + lane) + ri[a]]);
-            }
-#pragma unroll
-            for (int a = 0; a < 4; ++a) {
-                if (k0 == 0) {
-                    M[a] = fmaxf(M[a], ml[a].x);
-#pragma unroll
-                    for (int o = 16; o > 0; o >>= 1)
-                        M[a] = fmaxf(M[a], __shfl_xor_sync(0xffffffffu, M[a], o));
-                }
-                // (no weight: nothing was written)
-                w[a] = ml[a].x == -INFINITY && ml[a].y == 0.f ? 0.f
-                                                              : ex2((ml[a].x - M[a]) * p.scale_log2);
-                float s = w[a] * ml[a].y;
-#pragma unroll
-                for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-                l[a] += s;
-            }
-            const int n = min(32, sources - k0);
-#pragma unroll 2
-            for (int k = 0; k < n; ++k) {
-                float4 o[4];
-#pragma unroll
-                for (int a = 0; a < 4; ++a)
-                    o[a] = __ldcg(reinterpret_cast<const float4*>(
-                                      p.part + (int64_t)(base(k0 + k) + ri[a]) * kPagedDim) + lane);
-#pragma unroll
-                for (int a = 0; a < 4; ++a) {
-                    const float f = __shfl_sync(0xffffffffu, w[a], k);
-                    if (f == 0.f) continue;
-                    acc[a].x = fmaf(o[a].x, f, acc[a].x);
-                    acc[a].y = fmaf(o[a].y, f, acc[a].y);
-                    acc[a].z = fmaf(o[a].z, f, acc[a].z);
-                    acc[a].w = fmaf(o[a].w, f, acc[a].w);
-                }
+                const float f = staging[k * rows + min(rr + a, rows - 1)];
+                if (f == 0.f) continue;
+                acc[a].x = fmaf(o[a].x, f, acc[a].x);
+                acc[a].y = fmaf(o[a].y, f, acc[a].y);
+                acc[a].z = fmaf(o[a].z, f, acc[a].z);
+                acc[a].w = fmaf(o[a].w, f, acc[a].w);
             }
         }
 #pragma unroll
         for (int a = 0; a < 4; ++a) {
-            const int r = rr + a;
-            if (r >= r1) break;
-            const float inv = l[a] == 0.f ? 0.f : 1.f / l[a];
+            const int r = r0 + rr + a;
+            if (rr + a >= rows) break;
             *reinterpret_cast<uint2*>(
                 p.out + ((int64_t)(d.row0 + r / p.G) * p.Hq + d.g * p.G + r % p.G) * kPagedDim +
-                4 * lane) = make_uint2(Half16<BF>::pack(acc[a].x * inv, acc[a].y * inv),
-                                       Half16<BF>::pack(acc[a].z * inv, acc[a].w * inv));
+                4 * lane) = make_uint2(Half16<BF>::pack(acc[a].x, acc[a].y),
+                                       Half16<BF>::pack(acc[a].z, acc[a].w));
         }
     }
+    return meet(s, met);  // (the weights have been read)
+}
+
+// What becomes of a piece: its rows to out, to the workspace, or (narrow, of this CTA alone) the two
+// warpgroups' together to out.  (A function of its own: what it needs in registers would otherwise be
+// taken from the loop over the tiles.)
+template <bool BF>
+__device__ __noinline__ bool end_piece(const ChunkParams& p, Bars* s, uint8_t* staging, uint32_t tmem,
+                                       const Piece& x, bool first, float m, float l, uint32_t& met) {
+    const int wg = threadIdx.x >> 7, r = threadIdx.x & 127;
+    const uint32_t to = tmem + ((uint32_t)((threadIdx.x >> 5) & 3) << 21) + 256 + 128 * wg;
+    const float c = p.scale_log2;
+    const bool narrow = x.narrow;
+    const int per = p.tau * p.G;
+    const int r_item = narrow ? r : wg * per + r;
+    const bool valid = r < per && r_item < x.ntok * p.G;
+    const bool busy = __any_sync(0xffffffffu, valid);
+            uint8_t* orow = valid ? reinterpret_cast<uint8_t*>(
+                                        p.out + ((int64_t)(x.row0 + r_item / p.G) * p.Hq + x.g * p.G +
+                                                 r_item % p.G) * kPagedDim)
+                                  : nullptr;
+            const uint32_t mine = s32(staging) + (threadIdx.x >> 5) * 4096;
+            tc_after();
+            float inv = l == 0.f ? 0.f : 1.f / l;
+            if (x.nt == 0 || (!narrow && !x.split)) {  // (no token: nothing was summed)
+                for (int q = 0; busy && q < 2; ++q) {
+                    uint4 c[8] = {};
+                    if (!first) {
+    #pragma unroll
+                        for (int k = 0; k < 2; ++k) {
+                            float o[32];
+                            tm_ld32(to + 64 * q + 32 * k, o);
+                            tm_wait_ld();
+                            pin32(o);
+    #pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                c[4 * k + e] = pack8<BF>(o + 8 * e, inv);
+                        }
+                    }
+                    put_rows(mine, c, narrow && wg ? nullptr : orow ? orow + 128 * q : nullptr);
+                }
+            } else if (x.split) {  // the others' parts are looked for at the end of the share
+                const int64_t part =
+                    (2 * (int64_t)blockIdx.x + x.slot) * 2 * p.part_rows + wg * p.part_rows + r;
+                for (int q = 0; busy && !first && q < 4; ++q) {
+                    float o[32];
+                    tm_ld32(to + 32 * q, o);
+                    tm_wait_ld();
+                    pin32(o);
+                    uint4 c[8];
+    #pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        c[e] = make_uint4(__float_as_uint(o[4 * e]), __float_as_uint(o[4 * e + 1]),
+                                          __float_as_uint(o[4 * e + 2]), __float_as_uint(o[4 * e + 3]));
+                    put_rows(mine, c,
+                             valid ? reinterpret_cast<uint8_t*>(p.part + part * kPagedDim + 32 * q)
+                                   : nullptr);
+                }
+                if (valid) __stcg(&p.ml[part], make_float2(m, l));
+                __threadfence();
+                if (!meet(s, met)) return false;
+                if (threadIdx.x == 0) atomicAdd(&p.count[x.first], 1u);
+            } else {  // a narrow item of this CTA alone: the second warpgroup's sums by way of staging
+                float f0 = 0.f, f1 = 0.f;
+                for (int q = 0; q < 4; ++q) {
+                    float o[32];
+                    if (busy && !first) {
+                        tm_ld32(to + 32 * q, o);
+                        tm_wait_ld();
+                        pin32(o);
+                    }
+                    float4* slot = reinterpret_cast<float4*>(staging + (q & 1) * 16384 + r * 128);
+                    if (wg == 1) {
+                        if (q == 0) s->ml[r] = make_float2(m, l);
+                        if (busy && !first)
+    #pragma unroll
+                            for (int e = 0; e < 8; ++e)
+                                slot[e ^ (r & 7)] = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2],
+                                                                o[4 * e + 3]);
+                    }
+                    if (!meet(s, met)) return false;  // (two buffers: one meeting a round is enough)
+                    if (wg == 0 && busy) {
+                        if (q == 0) {
+                            const float2 b = s->ml[r];
+                            const float M = fmaxf(m, b.x);
+                            f0 = l == 0.f ? 0.f : ex2((m - M) * c);
+                            f1 = b.y == 0.f ? 0.f : ex2((b.x - M) * c);
+                            const float sum = fmaf(l, f0, b.y * f1);
+                            inv = sum == 0.f ? 0.f : 1.f / sum;
+                            f0 *= inv;
+                            f1 *= inv;
+                        }
+                        uint4 u[4];
+    #pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            float4 b = make_float4(0.f, 0.f, 0.f, 0.f);
+                            if (f1 != 0.f) b = slot[e ^ (r & 7)];
+                            o[4 * e] = fmaf(b.x, f1, o[4 * e] * f0);
+                            o[4 * e + 1] = fmaf(b.y, f1, o[4 * e + 1] * f0);
+                            o[4 * e + 2] = fmaf(b.z, f1, o[4 * e + 2] * f0);
+                            o[4 * e + 3] = fmaf(b.w, f1, o[4 * e + 3] * f0);
+                        }
+    #pragma unroll
+                        for (int e = 0; e < 4; ++e) u[e] = pack8<BF>(o + 8 * e, 1.f);
+                        if (valid)
+    #pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                *reinterpret_cast<uint4*>(orow + 64 * q + 16 * e) = u[e];
+                    }
+                    __syncwarp();
+                }
+                if (!meet(s, met)) return false;  // (staging is free again)
+            }
+            tc_before();  // (the next item's first product comes after the next P)
+    return true;
 }
 
 template <bool BF>
-__device__ void softmax_role(const ChunkParams& p, Bars* s, uint32_t tmem) {
+__device__ void softmax_role(const ChunkParams& p, Bars* s, uint8_t* staging, uint32_t tmem) {
     const int wg = threadIdx.x >> 7, r = threadIdx.x & 127;
     const uint32_t lanes = (uint32_t)((threadIdx.x >> 5) & 3) << 21;  // the warp's lanes of tensor memory
     const uint32_t ts = tmem + lanes + 128 * wg, to = tmem + lanes + 256 + 128 * wg;
@@ -752,54 +886,8 @@ __device__ void softmax_role(const ChunkParams& p, Bars* s, uint32_t tmem) {
             l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
         }
         if (!ok) break;
-        const int64_t orow = x.row0 + r_item / p.G;
-        const int ohead = x.g * p.G + r_item % p.G;
-        const bool direct = !narrow && !x.split;
-        if (x.nt == 0) {  // no row of the item sees a token
-            if (valid && !(narrow && wg)) {
-                float z[32];
-#pragma unroll
-                for (int e = 0; e < 32; ++e) z[e] = 0.f;
-                for (int q = 0; q < 4; ++q) store_row<BF>(p, orow, ohead, z, 32 * q, 0.f);
-            }
-        } else {
-            const int64_t part =
-                (2 * (int64_t)blockIdx.x + x.slot) * 2 * p.part_rows + wg * p.part_rows + r;
-            if (!first) {
-                if (!(ok = warp_wait(s, &s->o_full[wg], no++ & 1))) break;
-                tc_after();
-                const float inv = l == 0.f ? 0.f : 1.f / l;
-                for (int q = 0; busy && q < 4; ++q) {
-                    float o[32];
-                    tm_ld32(to + 32 * q, o);
-                    tm_wait_ld();
-                    pin32(o);
-                    if (valid && direct) {
-                        store_row<BF>(p, orow, ohead, o, 32 * q, inv);
-                    } else if (valid) {
-                        float4* dst = reinterpret_cast<float4*>(p.part + part * kPagedDim + 32 * q);
-#pragma unroll
-                        for (int e = 0; e < 8; ++e)
-                            __stcg(dst + e, make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2],
-                                                        o[4 * e + 3]));
-                    }
-                    __syncwarp();
-                }
-                tc_before();  // (the next item's first product comes after the next P)
-            }
-            if (!direct) {
-                if (valid) __stcg(&p.ml[part], make_float2(m, l));
-                if (x.split) {  // the others' parts are looked for at the end of the share
-                    __threadfence();
-                    if (!(ok = meet(s, met))) break;
-                    if (threadIdx.x == 0) atomicAdd(&p.count[x.first], 1u);
-                } else {        // a narrow item of this CTA alone
-                    if (!(ok = meet(s, met))) break;
-                    add_parts<BF>(p, x, 0, x.ntok * p.G);
-                    if (!(ok = meet(s, met))) break;
-                }
-            }
-        }
+        if (!first && !(ok = warp_wait(s, &s->o_full[wg], no++ & 1))) break;
+        if (!(ok = end_piece<BF>(p, s, staging, tmem, x, first, m, l, met))) break;
         __syncwarp();
         if ((threadIdx.x & 31) == 0) bar_arrive(&s->work_empty[w % kQueue]);
     }
@@ -823,7 +911,10 @@ __device__ void softmax_role(const ChunkParams& p, Bars* s, uint32_t tmem) {
         if (!(ok = meet(s, met)) || *(volatile uint32_t*)&s->abort) break;
         __threadfence();
         const long long rows = d.ntok * p.G;
-        add_parts<BF>(p, d, (int)(rows * d.index / d.parts), (int)(rows * (d.index + 1) / d.parts));
+        if (!(ok = add_parts<BF>(p, s, reinterpret_cast<float*>(staging), met, d,
+                                 (int)(rows * d.index / d.parts),
+                                 (int)(rows * (d.index + 1) / d.parts))))
+            break;
         if (threadIdx.x == 0) {  // the last to have seen the count clears it
             if (atomicAdd(&p.done[d.first], 1u) == (uint32_t)d.parts - 1) {
                 p.count[d.first] = 0;
@@ -875,12 +966,12 @@ __global__ void __launch_bounds__(kThreads, 1) paged_chunk_kernel(
     const uint32_t tmem = s->tmem;
     if (warp < 8) {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoft));
-        softmax_role<BF>(p, s, tmem);
+        softmax_role<BF>(p, s, raw + (smem - s32(raw)) + kStaging, tmem);
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsRest));
         if (warp == 8) load_role<BF>(p, s, smem);
         else if (threadIdx.x == 9 * 32) mma_role<BF>(p, s, smem, tmem);
-        else if (threadIdx.x == 10 * 32) walk_role(p, s);
+        else if (warp == 10) walk_role(p, s);
     }
     __syncwarp();
     tc_before();
@@ -929,7 +1020,6 @@ laq_status launch_chunk(const PagedKv& kv, bool bf, const void* q, int64_t q_str
     p.tau = 128 / p.G;
     p.T = T;
     p.max_q = max_q;
-    p.min_units = 4;
     p.part_rows = part_rows(max_q, p.G);
     p.scale_log2 = scale * 1.44269504088896340736f;
     p.out = static_cast<uint16_t*>(out);

@@ -21,7 +21,7 @@ struct ChunkParams {
     float* part;             // [CTA][2 slots][2 * part_rows][D]
     float2* ml;              // .. their (maximum, sum)
     uint32_t *status, *count, *done;
-    int G, Hq, tau, T, max_q, min_units, part_rows;
+    int G, Hq, tau, T, max_q, part_rows;
     float scale_log2;
 };
 
@@ -97,10 +97,25 @@ __device__ __forceinline__ float ex2(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-__host__ __device__ // The CTA whose share has unit u: shares start at floor(c W / ctas).
-__device__ __forceinline__ int cta_of(long long u, long long W, int ctas) {
-    return (int)(((u + 1) * ctas - 1) / W);
+__host__ __device__ // (64-bit division takes some hundred cycles: the sizes almost always fit 32 bits)
+__device__ __forceinline__ long long div_ll(long long a, long long b) {
+    return ((a | b) >> 32) == 0 ? (long long)((uint32_t)a / (uint32_t)b) : a / b;
 }
+// Equal shares of W units: the first `more` CTAs take each + 1 of them, the others `each`.
+struct Shares {
+    long long each, more;
+    __device__ __forceinline__ void set(long long W, int ctas) {
+        each = div_ll(W, ctas);
+        more = W - each * ctas;
+    }
+    __device__ __forceinline__ long long start(int cta) const {
+        return cta * each + min((long long)cta, more);
+    }
+    __device__ __forceinline__ int cta_of(long long u) const {
+        const long long big = more * (each + 1);
+        return (int)(u < big ? div_ll(u, each + 1) : more + div_ll(u - big, each));
+    }
+};
 
 }  // namespace
 }  // namespace laq

@@ -56,8 +56,8 @@ struct DecodeSmem {
     uint64_t full[kWarps][kSlots];
     uint32_t abort;
     int b, g, last;
-    long long at, u0, u1, W, scan[kWarps];
-    int ctas;
+    long long at, u0, u1, scan[kWarps];
+    Shares shares;
 };
 constexpr int kRing = kWarps * kSlots * kSlotBytes;
 constexpr int kSmem = kRing + 1024 + (int)sizeof(DecodeSmem);
@@ -133,7 +133,9 @@ __device__ void plan(const DecodeParams& p, DecodeSmem* s) {
     before += inc - sum;
     const int ctas = (int)min((long long)gridDim.x, W);
     if ((int)blockIdx.x >= ctas) return;
-    const long long u0 = W * blockIdx.x / ctas;
+    Shares sh;
+    sh.set(W, ctas);
+    const long long u0 = sh.start(blockIdx.x);
     if (u0 < before || u0 >= before + sum) return;
     int b = b0;
     long long at = before;
@@ -145,12 +147,11 @@ __device__ void plan(const DecodeParams& p, DecodeSmem* s) {
         at += (long long)units * p.kv.Hkv;
     }
     s->b = b;
-    s->g = (int)((u0 - at) / units);
+    s->g = (int)div_ll(u0 - at, units);
     s->at = at + (long long)s->g * units;
     s->u0 = u0;
-    s->u1 = W * (blockIdx.x + 1) / ctas;
-    s->W = W;
-    s->ctas = ctas;
+    s->u1 = sh.start(blockIdx.x + 1);
+    s->shares = sh;
 }
 
 template <bool BF, int NT>
@@ -410,7 +411,7 @@ __global__ void __launch_bounds__(kThreads, 2) paged_decode_kernel(
         }
         if (!whole) {
             if (tid < rows) __stcg(&p.ml[slot * p.part_rows + tid], s->ml[tid]);
-            const int first = cta_of(at, s->W, s->ctas), last = cta_of(at + units - 1, s->W, s->ctas);
+            const int first = s->shares.cta_of(at), last = s->shares.cta_of(at + units - 1);
             __threadfence();
             __syncthreads();
             if (tid == 0) {
