@@ -45,6 +45,7 @@ constexpr int kRegsSoft = 208, kRegsRest = 88;  // 2 * 208 + 88 = 3 * 168, the l
 constexpr int kQueue = 4;
 constexpr int kStaging = (2 + kStages) * kTileBytes;  // where: 4 KB for each softmax warp
 constexpr int kSmemTiles = kStaging + 8 * 4096;
+constexpr int kMostCtas = 192;          // so that a row of every part fits beside the others
 constexpr int kMinUnits = 4;            // fewer are not worth a CTA of their own
 constexpr int kStart = 2;               // what starting and ending an item costs, in tiles
 constexpr float kGrow = 8.f;            // how far a maximum may grow before O is rescaled (log2)
@@ -57,9 +58,21 @@ struct Piece {
     int split, slot, parts, index, first;  // of `parts` parts, the one `index`, of CTAs first ..
 };
 
+// What the functions that are not part of the loop need of the parameters: in shared memory, since a
+// reference to the parameters would be read through L2 there.
+struct Common {
+    uint16_t* out;
+    float* part;
+    float2* ml;
+    uint32_t* count;
+    int G, Hq, per, part_rows;
+    float scale_log2;
+};
+
 struct Bars {
+    Common c;
     uint64_t full[kStages], empty[kStages], q_full, q_empty, v_tail, drain;
-    uint64_t s_full[2], p_full[2], o_full[2], soft, work_full[kQueue], work_empty[kQueue];
+    uint64_t s_full[2], p_full[2], o_full[2], soft, fetch, work_full[kQueue], work_empty[kQueue];
     Piece queue[kQueue], pend[2];       // pieces in work; split ones that wait for their other parts
     uint32_t tmem, abort;
     int b;                              // this CTA's share: from unit `into` of request b, which starts at
@@ -215,36 +228,12 @@ struct Req {
         const int end = past + min(n, (t + 1) * 2 * p.tau);
         return (max(end, 0) + kTile - 1) / kTile;
     }
-    // tiles of the first x items (x < m): sum of ceil(max(0, past + (t + 1) 2 tau) / 128), as a sum of
-    // floors of a line, by Euclid's algorithm (every term fits 32 bits)
-    __device__ long long tiles_before(const ChunkParams& p, int x) const {
-        const uint32_t S = 2 * p.tau;
-        const uint32_t skip = past < 0 ? min((uint32_t)x, (uint32_t)(-(long long)past) / S) : 0;
-        long long sum = 0;
-        uint32_t n = x - skip, M = kTile, a = S,
-                 b = (uint32_t)(past + (int)((skip + 1) * S)) + kTile - 1;
-        while (n > 0) {
-            const uint32_t qa = a / M, qb = b / M;
-            sum += (long long)n * (n - 1) / 2 * qa + (long long)n * qb;
-            a -= qa * M;
-            b -= qb * M;
-            const uint32_t y = a * n + b;
-            if (y < M) break;
-            n = y / M;
-            b = y - n * M;
-            const uint32_t t = M;
-            M = a;
-            a = t;
-        }
-        return sum;
-    }
-    // the first unit of item t < m
-    __device__ long long start(const ChunkParams& p, int t) const {
-        return (long long)kStart * t + tiles_before(p, t);
-    }
     // units of all items of one kv head
     __device__ long long units(const ChunkParams& p) const {
-        return m == 0 ? 0 : start(p, m - 1) + kStart + tiles(p, m - 1);
+        long long sum = (long long)kStart * m;
+#pragma unroll 1
+        for (int t = 0; t < m; ++t) sum += tiles(p, t);
+        return sum;
     }
 };
 
@@ -255,6 +244,7 @@ __device__ void plan(const ChunkParams& p, Bars* s) {
     const int b0 = min(p.kv.batch, tid * per), b1 = min(p.kv.batch, b0 + per);
     Req r;
     long long sum = 0;
+#pragma unroll 1
     for (int b = b0; b < b1; ++b) {
         r.load(p, b);
         sum += r.units(p) * p.kv.Hkv;
@@ -269,6 +259,7 @@ __device__ void plan(const ChunkParams& p, Bars* s) {
     if (tid == 0) s->left = 0;
     __syncthreads();
     long long before = 0, W = 0;
+#pragma unroll 1
     for (int k = 0; k < kThreads / 32; ++k) {
         if (k < warp) before += s->scan[k];
         W += s->scan[k];
@@ -280,15 +271,15 @@ __device__ void plan(const ChunkParams& p, Bars* s) {
     sh.set(W, ctas);
     const long long u0 = sh.start(blockIdx.x);
     if (u0 < before || u0 >= before + sum) return;
-    for (int b = b0; b < b1; ++b) {
+    int b = b0;
+#pragma unroll 1
+    for (; b1 - b > 1; ++b) {  // (with one request a thread, it is that)
         r.load(p, b);
         const long long c = r.units(p) * p.kv.Hkv;
-        if (u0 < before + c) {
-            s->b = b;
-            break;
-        }
+        if (u0 < before + c) break;
         before += c;
     }
+    s->b = b;
     s->into = u0 - before;
     s->at = before;
     s->left = sh.start(blockIdx.x + 1) - u0;
@@ -305,18 +296,39 @@ __device__ void walk_role(const ChunkParams& p, Bars* s) {
     Req r;
     if (left > 0) {
         r.load(p, b);
-        long long into = s->into;
-        const long long per_head = r.units(p);
-        g = (int)div_ll(into, per_head);
-        into -= g * per_head;
-        for (int n = r.m; n > 1;) {  // the last of items t .. t + n - 1 that starts at or before `into`
-            const int step = (n + 31) / 32, at = (lane + 1) * step;
-            const int c = __popc(__ballot_sync(0xffffffffu, at < n && r.start(p, t + at) <= into));
-            t += c * step;
-            n = min(step, n - c * step);
+        long long into = s->into, per_head = 0;
+        // the warp adds up the items' units, 32 items at a time; a second time to find `into`
+#pragma unroll 1
+        for (int pass = 0, t0 = 0;;) {
+            int v = t0 + lane < r.m ? kStart + r.tiles(p, t0 + lane) : 0, inc = v;
+#pragma unroll 1
+            for (int o = 1; o < 32; o *= 2) {
+                const int y = __shfl_up_sync(0xffffffffu, inc, o);
+                if (lane >= o) inc += y;
+            }
+            const int all = __shfl_sync(0xffffffffu, inc, 31);
+            if (pass == 0) {
+                per_head += all;
+                if ((t0 += 32) < r.m) continue;
+                g = (int)div_ll(into, per_head);
+                into -= g * per_head;
+                U = s->at + g * per_head;
+                pass = 1;
+                t0 = 0;
+                if (r.m > 32) continue;
+            } else if (into >= all) {
+                into -= all;
+                U += all;
+                t0 += 32;
+                continue;
+            }
+            const int c = __popc(__ballot_sync(0xffffffffu, inc <= into && t0 + lane < r.m));
+            t = t0 + c;  // (its items before are counted in full)
+            const int start = __shfl_sync(0xffffffffu, inc - v, c);
+            off = (int)into - start;
+            U += start;
+            break;
         }
-        off = (int)(into - r.start(p, t));
-        U = s->at + g * per_head + into - off;
     }
     if (lane != 0) return;
     s->pend[0].nt = s->pend[1].nt = 0;
@@ -606,87 +618,98 @@ __device__ __forceinline__ void put_rows(uint32_t staging, const uint4 (&c)[8], 
 }
 
 // Add the parts of rows r0 .. r1 - 1 of a split item: part k is in slot (k == 0 ? 1 : 0) of CTA first + k,
-// a narrow item's as two halves of rows (the two warpgroups').  First the rows' weights, into staging, then
-// a warp takes four rows at a time, a lane four dimensions.
+// a narrow item's as two halves of rows (the two warpgroups').  The rows of a source lie in one piece: a
+// bulk copy a source brings them to where Q, K and V were (other SMs' fresh writes come at some 2000
+// cycles a round trip, and code that runs once is fetched at about 20 cycles an instruction: one wait and
+// little code).
 template <bool BF>
-__device__ __noinline__ bool add_parts(const ChunkParams& p, Bars* s, float* staging, uint32_t& met, const Piece& d,
-                          int r0, int r1) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int narrow = d.narrow, sources = narrow ? 2 * d.parts : d.parts, per = p.tau * p.G;
-    auto base = [&](int k) {  // first row of source k
+__device__ __noinline__ bool add_parts(Bars* s, uint32_t smem, uint8_t* tiles, uint32_t& met,
+                                       uint32_t& fetched, const Piece& d, int r0, int r1) {
+    const Common p = s->c;
+    const int narrow = d.narrow, sources = narrow ? 2 * d.parts : d.parts;
+    float* weight = reinterpret_cast<float*>(tiles + kStaging);  // [source][row]: 32 KB
+    const int most = min(kStaging / 512, 8192) / sources;        // rows at a time (sources <= 2 kMostCtas)
+    auto place = [&](int k, int r) {                             // of row r in source k
         const int part = narrow ? k >> 1 : k;
-        return (2 * (d.first + part) + (part == 0 ? 1 : 0)) * 2 * p.part_rows +
-               (narrow && (k & 1) ? p.part_rows : 0);
+        const int half = narrow ? k & 1 : r >= p.per;
+        return (2 * (d.first + part) + (part == 0 ? 1 : 0)) * 2 * p.part_rows + half * p.part_rows +
+               (half && !narrow ? r - p.per : r);
     };
-    auto row_in = [&](int r) { return narrow || r < per ? r : p.part_rows + r - per; };
-    const int rows = r1 - r0;  // (sources * rows fits: at most 2 * (256 + parts) floats)
-    if ((int)threadIdx.x < rows) {
-        const int ri = row_in(r0 + threadIdx.x);
-        float M = -INFINITY, l = 0.f;
-#pragma unroll 8
-        for (int k = 0; k < sources; ++k) M = fmaxf(M, __ldcg(&p.ml[base(k) + ri]).x);
-#pragma unroll 8
-        for (int k = 0; k < sources; ++k) {
-            const float2 ml = __ldcg(&p.ml[base(k) + ri]);
-            // (no weight: nothing was written)
-            const float f =
-                ml.x == -INFINITY && ml.y == 0.f ? 0.f : ex2((ml.x - M) * p.scale_log2);
-            staging[k * rows + threadIdx.x] = f;
-            l = fmaf(f, ml.y, l);
+    const int tid = threadIdx.x;
+#pragma unroll 1
+    for (int rows; r0 < r1; r0 += rows) {
+        rows = min(r1 - r0, most);
+        if (!narrow && r0 < p.per) rows = min(rows, p.per - r0);
+        if (tid < 32) {
+            asm volatile("fence.proxy.async;" ::: "memory");  // (the copies come after the parts' count)
+            if (tid == 0) bar_expect(&s->fetch, sources * rows * 512);
+            __syncwarp();
+#pragma unroll 1
+            for (int k = tid; k < sources; k += 32)
+                asm volatile(
+                    "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, "
+                    "[%3];" ::"r"(smem + k * rows * 512),
+                    "l"(p.part + (int64_t)place(k, r0) * kPagedDim), "r"(rows * 512),
+                    "r"(s32(&s->fetch))
+                    : "memory");
         }
-        const float inv = l == 0.f ? 0.f : 1.f / l;
-        for (int k = 0; k < sources; ++k) staging[k * rows + threadIdx.x] *= inv;
-    }
-    if (!meet(s, met)) return false;
-    for (int rr = 4 * warp; rr < rows; rr += 32) {
-        int ri[4];  // the rows' places in a part
-        float4 acc[4];
-#pragma unroll
-        for (int a = 0; a < 4; ++a) {
-            ri[a] = row_in(r0 + min(rr + a, rows - 1));
-            acc[a] = make_float4(0.f, 0.f, 0.f, 0.f);
-        }
+        if (tid < rows) {
+            float M = -INFINITY, l = 0.f;
 #pragma unroll 4
-        for (int k = 0; k < sources; ++k) {
-            float4 o[4];
-            const float4* src = reinterpret_cast<const float4*>(p.part) +
-                                (int64_t)base(k) * (kPagedDim / 4) + lane;
-#pragma unroll
-            for (int a = 0; a < 4; ++a) o[a] = __ldcg(src + ri[a] * (kPagedDim / 4));
-#pragma unroll
-            for (int a = 0; a < 4; ++a) {
-                const float f = staging[k * rows + min(rr + a, rows - 1)];
-                if (f == 0.f) continue;
-                acc[a].x = fmaf(o[a].x, f, acc[a].x);
-                acc[a].y = fmaf(o[a].y, f, acc[a].y);
-                acc[a].z = fmaf(o[a].z, f, acc[a].z);
-                acc[a].w = fmaf(o[a].w, f, acc[a].w);
+            for (int k = 0; k < sources; ++k) M = fmaxf(M, __ldcg(&p.ml[place(k, r0 + tid)]).x);
+#pragma unroll 1
+            for (int k = 0; k < sources; ++k) {
+                const float2 v = __ldcg(&p.ml[place(k, r0 + tid)]);
+                // (no weight: nothing was written)
+                const float f =
+                    v.x == -INFINITY && v.y == 0.f ? 0.f : ex2((v.x - M) * p.scale_log2);
+                weight[k * rows + tid] = f;
+                l = fmaf(f, v.y, l);
             }
+            const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll 1
+            for (int k = 0; k < sources; ++k) weight[k * rows + tid] *= inv;
         }
-#pragma unroll
-        for (int a = 0; a < 4; ++a) {
-            const int r = r0 + rr + a;
-            if (rr + a >= rows) break;
+        const uint32_t turn = fetched++ & 1;
+        if (!meet(s, met) || !warp_wait(s, &s->fetch, turn)) {
+            drain(&s->fetch, turn);
+            return false;
+        }
+#pragma unroll 1
+        for (int e = tid; e < rows * 32; e += 256) {
+            const int row = e >> 5, r = r0 + row;
+            float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 2
+            for (int k = 0; k < sources; ++k) {
+                const float f = weight[k * rows + row];
+                const float4 o = reinterpret_cast<const float4*>(tiles)[(k * rows + row) * 32 + (e & 31)];
+                if (f == 0.f) continue;
+                a.x = fmaf(o.x, f, a.x);
+                a.y = fmaf(o.y, f, a.y);
+                a.z = fmaf(o.z, f, a.z);
+                a.w = fmaf(o.w, f, a.w);
+            }
             *reinterpret_cast<uint2*>(
                 p.out + ((int64_t)(d.row0 + r / p.G) * p.Hq + d.g * p.G + r % p.G) * kPagedDim +
-                4 * lane) = make_uint2(Half16<BF>::pack(acc[a].x, acc[a].y),
-                                       Half16<BF>::pack(acc[a].z, acc[a].w));
+                4 * (e & 31)) = make_uint2(Half16<BF>::pack(a.x, a.y), Half16<BF>::pack(a.z, a.w));
         }
+        if (!meet(s, met)) return false;  // (the rows have been read)
     }
-    return meet(s, met);  // (the weights have been read)
+    return true;
 }
 
 // What becomes of a piece: its rows to out, to the workspace, or (narrow, of this CTA alone) the two
 // warpgroups' together to out.  (A function of its own: what it needs in registers would otherwise be
 // taken from the loop over the tiles.)
 template <bool BF>
-__device__ __noinline__ bool end_piece(const ChunkParams& p, Bars* s, uint8_t* staging, uint32_t tmem,
+__device__ __noinline__ bool end_piece(Bars* s, uint8_t* staging, uint32_t tmem,
                                        const Piece& x, bool first, float m, float l, uint32_t& met) {
     const int wg = threadIdx.x >> 7, r = threadIdx.x & 127;
     const uint32_t to = tmem + ((uint32_t)((threadIdx.x >> 5) & 3) << 21) + 256 + 128 * wg;
+    const Common p = s->c;
     const float c = p.scale_log2;
     const bool narrow = x.narrow;
-    const int per = p.tau * p.G;
+    const int per = p.per;
     const int r_item = narrow ? r : wg * per + r;
     const bool valid = r < per && r_item < x.ntok * p.G;
     const bool busy = __any_sync(0xffffffffu, valid);
@@ -734,7 +757,7 @@ __device__ __noinline__ bool end_piece(const ChunkParams& p, Bars* s, uint8_t* s
                 if (valid) __stcg(&p.ml[part], make_float2(m, l));
                 __threadfence();
                 if (!meet(s, met)) return false;
-                if (threadIdx.x == 0) atomicAdd(&p.count[x.first], 1u);
+                if (threadIdx.x == 0) atomicAdd(&s->c.count[x.first], 1u);
             } else {  // a narrow item of this CTA alone: the second warpgroup's sums by way of staging
                 float f0 = 0.f, f1 = 0.f;
                 for (int q = 0; q < 4; ++q) {
@@ -791,12 +814,13 @@ __device__ __noinline__ bool end_piece(const ChunkParams& p, Bars* s, uint8_t* s
 }
 
 template <bool BF>
-__device__ void softmax_role(const ChunkParams& p, Bars* s, uint8_t* staging, uint32_t tmem) {
+__device__ void softmax_role(const ChunkParams& p, Bars* s, uint32_t smem, uint8_t* staging,
+                             uint32_t tmem) {
     const int wg = threadIdx.x >> 7, r = threadIdx.x & 127;
     const uint32_t lanes = (uint32_t)((threadIdx.x >> 5) & 3) << 21;  // the warp's lanes of tensor memory
     const uint32_t ts = tmem + lanes + 128 * wg, to = tmem + lanes + 256 + 128 * wg;
     const float c = p.scale_log2, offset = BF ? 0.f : 7.f;
-    uint32_t ns = 0, no = 0, met = 0;
+    uint32_t ns = 0, no = 0, met = 0, fetched = 0;
     bool ok = true;
     for (uint32_t w = 0; ok; ++w) {
         if (!(ok = warp_wait(s, &s->work_full[w % kQueue], (w / kQueue) & 1))) break;
@@ -887,7 +911,7 @@ __device__ void softmax_role(const ChunkParams& p, Bars* s, uint8_t* staging, ui
         }
         if (!ok) break;
         if (!first && !(ok = warp_wait(s, &s->o_full[wg], no++ & 1))) break;
-        if (!(ok = end_piece<BF>(p, s, staging, tmem, x, first, m, l, met))) break;
+        if (!(ok = end_piece<BF>(s, staging, tmem, x, first, m, l, met))) break;
         __syncwarp();
         if ((threadIdx.x & 31) == 0) bar_arrive(&s->work_empty[w % kQueue]);
     }
@@ -910,10 +934,10 @@ __device__ void softmax_role(const ChunkParams& p, Bars* s, uint8_t* staging, ui
         }
         if (!(ok = meet(s, met)) || *(volatile uint32_t*)&s->abort) break;
         __threadfence();
-        const long long rows = d.ntok * p.G;
-        if (!(ok = add_parts<BF>(p, s, reinterpret_cast<float*>(staging), met, d,
-                                 (int)(rows * d.index / d.parts),
-                                 (int)(rows * (d.index + 1) / d.parts))))
+        const int rows = d.ntok * p.G;
+        if (!(ok = add_parts<BF>(s, smem, staging - kStaging, met, fetched, d,
+                                 rows * d.index / d.parts,
+                                 rows * (d.index + 1) / d.parts)))
             break;
         if (threadIdx.x == 0) {  // the last to have seen the count clears it
             if (atomicAdd(&p.done[d.first], 1u) == (uint32_t)d.parts - 1) {
@@ -940,6 +964,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_chunk_kernel(
         bar_init(&s->q_empty, 1);
         bar_init(&s->v_tail, 1);
         bar_init(&s->drain, 1);
+        bar_init(&s->fetch, 1);
         bar_init(&s->soft, 8);
         for (int i = 0; i < kQueue; ++i) {
             bar_init(&s->work_full[i], 1);
@@ -951,6 +976,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_chunk_kernel(
             bar_init(&s->o_full[i], 1);
         }
         s->abort = 0;
+        s->c = Common{p.out, p.part, p.ml, p.count, p.G, p.Hq, p.tau * p.G, p.part_rows, p.scale_log2};
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 9) {
@@ -966,7 +992,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_chunk_kernel(
     const uint32_t tmem = s->tmem;
     if (warp < 8) {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoft));
-        softmax_role<BF>(p, s, raw + (smem - s32(raw)) + kStaging, tmem);
+        softmax_role<BF>(p, s, smem, raw + (smem - s32(raw)) + kStaging, tmem);
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsRest));
         if (warp == 8) load_role<BF>(p, s, smem);
@@ -1010,7 +1036,7 @@ laq_status launch_chunk(const PagedKv& kv, bool bf, const void* q, int64_t q_str
             cudaFuncSetAttribute((const void*)paged_chunk_kernel<false>,
                                  cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem) != cudaSuccess)
             return LAQ_ERR_CUDA;
-        if (sms > kPartCtas) sms = kPartCtas;
+        if (sms > kMostCtas) sms = kMostCtas;
         sms_of[dev].store(sms);
     }
     ChunkParams p = {};
