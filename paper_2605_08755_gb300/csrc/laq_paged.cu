@@ -96,17 +96,17 @@ namespace {
 
 // ---- append ----
 // One half-warp per head vector: lane l of 16 holds elements 4l .. 4l+3 and 64 + 4l .. 64 + 4l+3, the
-// two sides of four rotation pairs, so the norm is four shuffles and the rotation none.  A CTA takes
-// kTokens tokens (or some of the heads of one token, where there are few): one warp finds each token's request, position
-// and slot, one thread turns each (token, frequency), then the half-warps walk the CTA's head vectors,
-// kAhead of them loaded before anything waits.
+// two sides of four rotation pairs, so the norm is four shuffles and the rotation none.  A CTA takes TOK
+// tokens and heads_per_cta heads: one warp finds each token's request, position and slot, one thread
+// turns each (token, frequency), then a half-warp takes a head of all TOK tokens at a time, the next
+// one's vectors in flight meanwhile.
 //   The angle p * theta^(-2i/D) is reduced in whole turns first: turn[i] = theta^(-2i/D) / 2 pi as a
 // 64-bit fraction, so p * turn[i] mod 2^64 is the fraction of a turn to 2^-64 p, whatever p (an fp32
 // product is off by 2^-24 of the angle: 2e-3 radians at position 40,000).
 //   Bound: HBM (each head vector read and written once); for few tokens the chain request -> length ->
 // page -> store, about four dependent loads.
 constexpr int kAppendThreads = 256;
-constexpr int kAhead = 4;
+constexpr int kHeadsAtOnce = kAppendThreads / 16;
 
 struct AppendParams {
     PagedKv kv;
@@ -114,41 +114,37 @@ struct AppendParams {
     const uint16_t *qw, *kw;
     uint16_t* q_out;
     int64_t qkv_stride;
-    int T, Hq, tokens, heads_per_cta;
+    int T, Hq, heads_per_cta;
     float eps;
     uint64_t turn[kPagedDim / 2];
 };
 
-template <bool BF>
-__global__ void __launch_bounds__(kAppendThreads) paged_append_kernel(
+// CTAS: resident per SM
+template <bool BF, int TOK, int CTAS>
+__global__ void __launch_bounds__(kAppendThreads, CTAS) paged_append_kernel(
     const __grid_constant__ AppendParams p) {
     using H = Half16<BF>;
-    constexpr int kTok = 4;
-    __shared__ float4 cs[kTok][kPagedDim / 8], sn[kTok][kPagedDim / 8];
-    __shared__ int pos_s[kTok];        // position
-    __shared__ int64_t slot_s[kTok];   // element offset of the slot (head 0), -1: none; -2: no request
+    __shared__ float4 cs[TOK][kPagedDim / 8], sn[TOK][kPagedDim / 8];
+    __shared__ int pos_s[TOK];        // position
+    __shared__ int64_t slot_s[TOK];   // element offset of the slot (head 0), -1: none; -2: no request
     pdl_launch_dependents();
     pdl_wait();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int t0 = blockIdx.x * p.tokens, nt = min(p.tokens, p.T - t0);
-    const int nh = p.Hq + 2 * p.kv.Hkv, h0 = blockIdx.y * p.heads_per_cta;
-    const int heads = min(p.heads_per_cta, nh - h0), rows = nt * heads;
-    const int hw = threadIdx.x >> 4, l = threadIdx.x & 15;
-    constexpr int kStride = kAppendThreads / 16;
-    uint2 lo[kAhead], hi[kAhead];
-    auto load = [&](int r0) {
+    const int t0 = blockIdx.x * TOK, nt = min(TOK, p.T - t0);
+    const int h_end = min(p.Hq + 2 * p.kv.Hkv, (int)(blockIdx.y + 1) * p.heads_per_cta);
+    const int l = threadIdx.x & 15;
+    int h = blockIdx.y * p.heads_per_cta + (threadIdx.x >> 4);
+    uint2 lo[TOK], hi[TOK];
+    auto load = [&] {
+        const uint16_t* src = p.qkv + (int64_t)t0 * p.qkv_stride + h * kPagedDim + 4 * l;
 #pragma unroll
-        for (int a = 0; a < kAhead; ++a) {
-            const int r = r0 + a * kStride;
-            if (r < rows) {
-                const uint16_t* src = p.qkv + (int64_t)(t0 + r / heads) * p.qkv_stride +
-                                      (int64_t)(h0 + r % heads) * kPagedDim + 4 * l;
-                lo[a] = *reinterpret_cast<const uint2*>(src);
-                hi[a] = *reinterpret_cast<const uint2*>(src + 64);
+        for (int t = 0; t < TOK; ++t, src += p.qkv_stride)
+            if (t < nt) {
+                lo[t] = *reinterpret_cast<const uint2*>(src);
+                hi[t] = *reinterpret_cast<const uint2*>(src + 64);
             }
-        }
     };
-    load(hw);
+    if (h < h_end) load();
     if (warp < nt) {
         const int t = t0 + warp, b = request_of(p.kv.q_start, p.kv.batch, t);
         const int s0 = b < p.kv.batch ? p.kv.q_start[b] : 0x7fffffff;
@@ -182,50 +178,49 @@ __global__ void __launch_bounds__(kAppendThreads) paged_append_kernel(
         reinterpret_cast<float*>(cs[t])[i] = c;
         reinterpret_cast<float*>(sn[t])[i] = s;
     }
-    float wq[8], wk[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) wq[e] = wk[e] = 1.f;
-    auto weights = [&](const uint16_t* w, float (&o)[8]) {
-        if (!w) return;
-#pragma unroll
-        for (int side = 0; side < 2; ++side) {
-            const uint2 u = *reinterpret_cast<const uint2*>(w + 64 * side + 4 * l);
-            const float2 a = H::unpack(u.x), b = H::unpack(u.y);
-            o[4 * side] = a.x; o[4 * side + 1] = a.y; o[4 * side + 2] = b.x; o[4 * side + 3] = b.y;
-        }
-    };
-    weights(p.qw, wq);
-    weights(p.kw, wk);
     __syncthreads();
-    for (int r0 = hw; r0 < rows; r0 += kAhead * kStride) {
-        if (r0 != hw) load(r0);
+    const unsigned half = 0xffffu << (threadIdx.x & 16);  // (the two halves of a warp part at the end)
+    while (h < h_end) {
+        const bool is_q = h < p.Hq, is_v = h >= p.Hq + p.kv.Hkv;
+        const uint16_t* wp = is_v ? nullptr : is_q ? p.qw : p.kw;
+        float w[8];
+        if (wp) {
 #pragma unroll
-        for (int a = 0; a < kAhead; ++a) {
-            const int r = r0 + a * kStride;
-            // (the lanes of a half-warp leave together; the other half may stay: the shuffles below
-            // name the half's own lanes)
-            if (r >= rows) break;
-            const int t = r / heads, h = h0 + r % heads;
+            for (int side = 0; side < 2; ++side) {
+                const uint2 u = *reinterpret_cast<const uint2*>(wp + 64 * side + 4 * l);
+                const float2 a = H::unpack(u.x), b = H::unpack(u.y);
+                w[4 * side] = a.x; w[4 * side + 1] = a.y; w[4 * side + 2] = b.x; w[4 * side + 3] = b.y;
+            }
+        }
+        uint2 ol[TOK], oh[TOK];
+#pragma unroll
+        for (int t = 0; t < TOK; ++t) {
+            ol[t] = lo[t];
+            oh[t] = hi[t];
+        }
+        const int head = h;
+        h += kHeadsAtOnce;
+        if (h < h_end) load();
+#pragma unroll
+        for (int t = 0; t < TOK; ++t) {
+            if (t >= nt) break;
             const int64_t slot = slot_s[t];
             if (slot == -2) continue;
-            const bool is_q = h < p.Hq, is_v = h >= p.Hq + p.kv.Hkv;
-            uint2 ol = lo[a], oh = hi[a];
             if (!is_v) {
                 float x[8];
-                const float2 f0 = H::unpack(lo[a].x), f1 = H::unpack(lo[a].y),
-                             f2 = H::unpack(hi[a].x), f3 = H::unpack(hi[a].y);
+                const float2 f0 = H::unpack(ol[t].x), f1 = H::unpack(ol[t].y),
+                             f2 = H::unpack(oh[t].x), f3 = H::unpack(oh[t].y);
                 x[0] = f0.x; x[1] = f0.y; x[2] = f1.x; x[3] = f1.y;
                 x[4] = f2.x; x[5] = f2.y; x[6] = f3.x; x[7] = f3.y;
-                if (is_q ? p.qw != nullptr : p.kw != nullptr) {
+                if (wp) {
                     float ss = 0.f;
 #pragma unroll
                     for (int e = 0; e < 8; ++e) ss = fmaf(x[e], x[e], ss);
-                    const unsigned half = 0xffffu << (threadIdx.x & 16);
 #pragma unroll
                     for (int o = 8; o > 0; o >>= 1) ss += __shfl_xor_sync(half, ss, o);
-                    const float inv = rsqrtf(ss / (float)kPagedDim + p.eps);
+                    const float inv = rsqrtf(ss * (1.f / kPagedDim) + p.eps);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) x[e] = x[e] * inv * (is_q ? wq[e] : wk[e]);
+                    for (int e = 0; e < 8; ++e) x[e] = x[e] * inv * w[e];
                 }
                 const float4 c4 = cs[t][l], s4 = sn[t][l];
                 const float c[4] = {c4.x, c4.y, c4.z, c4.w}, s[4] = {s4.x, s4.y, s4.z, s4.w};
@@ -235,21 +230,32 @@ __global__ void __launch_bounds__(kAppendThreads) paged_append_kernel(
                     y[e] = x[e] * c[e] - x[4 + e] * s[e];
                     y[4 + e] = x[4 + e] * c[e] + x[e] * s[e];
                 }
-                ol = make_uint2(H::pack(y[0], y[1]), H::pack(y[2], y[3]));
-                oh = make_uint2(H::pack(y[4], y[5]), H::pack(y[6], y[7]));
+                ol[t] = make_uint2(H::pack(y[0], y[1]), H::pack(y[2], y[3]));
+                oh[t] = make_uint2(H::pack(y[4], y[5]), H::pack(y[6], y[7]));
             }
             uint16_t* dst;
             if (is_q) {
-                dst = p.q_out + ((int64_t)(t0 + t) * p.Hq + h) * kPagedDim;
+                dst = p.q_out + ((int64_t)(t0 + t) * p.Hq + head) * kPagedDim;
             } else {
                 if (slot < 0) continue;
-                const int g = h - p.Hq - (is_v ? p.kv.Hkv : 0);
+                const int g = head - p.Hq - (is_v ? p.kv.Hkv : 0);
                 dst = (is_v ? p.kv.v : p.kv.k) + slot + (int64_t)g * p.kv.head_stride;
             }
-            *reinterpret_cast<uint2*>(dst + 4 * l) = ol;
-            *reinterpret_cast<uint2*>(dst + 64 + 4 * l) = oh;
+            *reinterpret_cast<uint2*>(dst + 4 * l) = ol[t];
+            *reinterpret_cast<uint2*>(dst + 64 + 4 * l) = oh[t];
         }
     }
+}
+
+template <bool BF>
+void (*append_kernel(int64_t T, int* tok))(const AppendParams) {
+    // One token a CTA up to a wave of four CTAs an SM (152 SMs), then two; past the second wave's worth five
+    // CTAs an SM, whose third wave of four would leave SMs idle.  Measured, 48 heads, us at 1 / 2 (4 CTAs)
+    // / 2 (5) tokens a CTA: 600 tokens 4.7 / 6.2 / 8.3, 1000 7.8 / 6.8 / 8.7, 1500 12.4 / 11.6 / 10.1,
+    // 8192 52.1 / 41.3 / 40.6 (four tokens: 43.2; vectors by way of shared memory, more in flight: 44.7).
+    *tok = T <= 608 ? 1 : 2;
+    return T <= 608 ? paged_append_kernel<BF, 1, 4>
+           : T <= 1216 ? paged_append_kernel<BF, 2, 4> : paged_append_kernel<BF, 2, 5>;
 }
 
 template <typename P>
@@ -299,13 +305,13 @@ laq_status laq_paged_append(const laq_paged_kv* kv, const void* qkv, int64_t qkv
     const double ratio = pow((double)theta, -2.0 / kPagedDim);
     double f = 0.15915494309189533577 * 0x1p64;  // 2^64 / (2 pi)
     for (int i = 0; i < kPagedDim / 2; ++i, f *= ratio) p.turn[i] = (uint64_t)f;
-    p.tokens = 4;
-    p.heads_per_cta = nh;
-    const dim3 grid((unsigned)((T + p.tokens - 1) / p.tokens),
+    int tok = 1;
+    const auto kernel = kv->dtype == LAQ_BF16 ? append_kernel<true>(T, &tok) : append_kernel<false>(T, &tok);
+    // (few tokens: 16 heads a CTA, a head vector for every half-warp; 200 tokens 4.4 -> 3.2 us)
+    p.heads_per_cta = T <= 256 ? kHeadsAtOnce : nh;
+    const dim3 grid((unsigned)((T + tok - 1) / tok),
                     (unsigned)((nh + p.heads_per_cta - 1) / p.heads_per_cta));
-    return kv->dtype == LAQ_BF16
-               ? launch_paged(paged_append_kernel<true>, grid, kAppendThreads, stream, p)
-               : launch_paged(paged_append_kernel<false>, grid, kAppendThreads, stream, p);
+    return launch_paged(kernel, grid, kAppendThreads, stream, p);
 }
 
 size_t laq_paged_attention_workspace_bytes(int64_t T, int64_t batch, int64_t max_q, int32_t Hq,
