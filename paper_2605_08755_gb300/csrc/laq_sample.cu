@@ -4,25 +4,30 @@
 // Weights are whole numbers (2^40 for the maximum), so that every sum is exact, integer atomics give
 // one result in any order, and no result depends on how a row is split.  What top-k and top-p keep is
 // a prefix of the order (logit descending, index ascending), found in three steps:
-//   1. a histogram of the row in 2048 bins of equal width below its maximum (of counts for top-k; of
-//      weights and counts for top-p), whose prefix sums name the bin that the cut falls in;
+//   1. a histogram in 2048 bins of equal width below the row's maximum, whose prefix sums name the bin
+//      that the cut falls in.  For top-p: of every logit's weight and count.  For a small top-k: of the
+//      maxima that the threads have found, one each; where k of them lie above an edge, at least k
+//      logits do, and hardly more; else of every logit's count;
 //   2. the elements of that bin, or, where the whole prefix up to it is small (the usual case), all
-//      elements up to it, are gathered into a list and sorted;
-//   3. prefix sums over the sorted list give the cut to the element.
+//      elements up to it, are gathered into a list;
+//   3. the list is ranked (by comparing all pairs, or sorted where it is long), and prefix sums in that
+//      order give the cut to the element.
 // A list that would not fit is refined by further histograms of the elements' keys (order-preserving
 // bits of the logit, then of the index).  With the whole prefix in the list the token is chosen there;
 // otherwise a last pass sums the kept weights in the order of the index.
 //
 // A cluster of C CTAs works on a row, each on a slice that it reads once and keeps in shared memory
-// (a slice that does not fit is read again, from L2).  Histograms meet by distributed shared memory,
-// the list lies in CTA 0.
+// (a slice that does not fit is read again, from L2).  Histograms and the list meet in CTA 0, by
+// distributed shared memory.
 // The quotient (x - top) / t costs a compiler's division ten instructions for each logit; a row's t is
 // one number, so it is formed from the rounded reciprocal with one correction (Markstein, IBM J. Res.
-// Dev. 34, 1990), which gives the correctly rounded quotient.
+// Dev. 34, 1990), which gives the correctly rounded quotient.  A weight's whole number is its float's
+// significand, shifted: the conversion instruction to 64 bits runs on the few fp64 units.
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
+#include <float.h>
 #include <stdint.h>
 
 #include <atomic>
@@ -42,6 +47,8 @@ constexpr int kList = 2048;        // elements of the list
 constexpr int kIdxBits = 22;       // V <= 2^22
 constexpr int kMaxWarps = 32;
 constexpr int kMaxC = 8;
+constexpr int kPairs = 256;        // lists up to this are ranked by comparing all pairs
+constexpr int kSmallK = 512;       // top-k up to this starts from the threads' maxima
 
 struct SampleParams {
     const void* logits;
@@ -54,13 +61,18 @@ struct SampleParams {
 };
 
 struct SampleSmem {
-    uint32_t cnt[kBins], lo[kBins], hi[kBins];
+    union {
+        struct {
+            uint32_t cnt[kBins], lo[kBins], hi[kBins];
+        };
+        u64 w[kList];            // the list's weights, once the bins are done with
+    };
     u64 list[kList];
     u64 red[kMaxWarps], red2[kMaxWarps];
     float fred[2][kMaxWarps];
     float2 ends[kMaxC];          // (max, min) of every CTA of the cluster
     u64 sums[kMaxC];             // kept weight of every CTA
-    u64 found[4], cut;
+    u64 found[5], cut, part_of;
     uint32_t n_list, first;
 };
 
@@ -103,7 +115,7 @@ struct Logits<LAQ_F16> : Logits16<false> {};
 template <>
 struct Logits<LAQ_BF16> : Logits16<true> {};
 
-__device__ __forceinline__ float clean(float x) { return isnan(x) ? -INFINITY : x + 0.f; }
+__device__ __forceinline__ float clean(float x) { return fmaxf(x, -INFINITY) + 0.f; }
 
 // order-preserving key of a logit, and back
 __device__ __forceinline__ uint32_t key_of(float x) {
@@ -142,8 +154,10 @@ struct Weights {
             q = fmaxf(d * r, -64.f);  // (past -28 the weight is 0: the bound keeps -inf apart from +inf)
             q = fmaf(fmaf(-q, t, d), r, q);
         }
-        const u64 w = (u64)(expf(q) * 0x1p40f);
-        return x == top ? (u64)1 << 40 : w;
+        // floor(e * 2^40) of e = significand * 2^(exponent - 23), e <= 1 (a NaN, of infinite t, is 0)
+        const uint32_t e = __float_as_uint(expf(q));
+        const u64 w = (u64)((e & 0x7fffffu) | 0x800000u) << 17 >> min(127u - min(e >> 23, 127u), 63u);
+        return x == top ? (u64)1 << 40 : e < 0x7f800000u ? w : 0;
     }
 };
 
@@ -205,16 +219,19 @@ __device__ __forceinline__ u64 block_scan(u64 v, u64* red, u64* total) {
     return before + inc - v;
 }
 
-// Sort the first n of list, padded to a power of two with `pad`; descending or ascending.
-__device__ __forceinline__ void sort_list(u64* list, int n, bool descending) {
+// Sort the first n of list (padded to a power of two), descending or ascending.
+__device__ __noinline__ void sort_list(u64* list, int n, bool descending) {
     int N = 32;
     while (N < n) N *= 2;
     for (int i = n + threadIdx.x; i < N; i += blockDim.x) list[i] = descending ? 0 : ~(u64)0;
+#pragma unroll 1
     for (int k = 2; k <= N; k *= 2)
+#pragma unroll 1
         for (int j = k / 2; j > 0; j /= 2) {
             __syncthreads();
+#pragma unroll 1
             for (int i = threadIdx.x; i < N / 2; i += blockDim.x) {
-                const int a = (i / j) * 2 * j + i % j, b = a + j;
+                const int a = 2 * i - (i & (j - 1)), b = a + j;
                 const u64 x = list[a], y = list[b];
                 const bool up = ((a & k) == 0) != descending;  // this run ascends
                 if ((x > y) == up) {
@@ -233,6 +250,7 @@ __global__ void __launch_bounds__(1024) sample_kernel(const SampleParams p) {
     uint8_t* slice = dyn + sizeof(SampleSmem);
     static_assert(sizeof(SampleSmem) % 16 == 0, "the slice is 16-byte aligned");
     pdl_launch_dependents();
+    if (p.C > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;\n" ::: "memory");
     cg::cluster_group cluster = cg::this_cluster();
     const int C = p.C, rank = C > 1 ? (int)cluster.block_rank() : 0;
     const int tid = threadIdx.x, nt = blockDim.x, warp = tid >> 5, lane = tid & 31;
@@ -281,6 +299,7 @@ __global__ void __launch_bounds__(1024) sample_kernel(const SampleParams p) {
             row.aligned = true;
         }
     }
+    const float thread_top = top;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
@@ -309,7 +328,7 @@ __global__ void __launch_bounds__(1024) sample_kernel(const SampleParams p) {
         }
     }
     // (every CTA of the cluster has to have started before its shared memory is written)
-    if (C > 1) cluster.sync();
+    if (C > 1) asm volatile("barrier.cluster.wait.aligned;\n" ::: "memory");
     if (warp == 0 && lane < C) remote(&s.ends[0], lane)[rank] = make_float2(top, bot);
     all_sync();
     top = -INFINITY, bot = INFINITY;
@@ -361,71 +380,91 @@ __global__ void __launch_bounds__(1024) sample_kernel(const SampleParams p) {
         const uint32_t up = (uint32_t)(w >> 32) + (old + wl < old);
         if (up) atomicAdd(&s.hi[b], up);
     };
-    // The cluster's bins: prefix sums of counts or weights; the bin where they reach `need` (all
-    // threads of all CTAs get the same).  found: bin, what is left of `need` in it, the elements of the
-    // bin, the elements up to and with it.  Returns the sum over all bins.  *need may depend on that sum.
+    // The cluster's bins, added up in CTA 0: prefix sums of counts or weights, and the bin where they
+    // reach need_of(sum over all bins).  found, in all CTAs: bin, what is left of the need in it, the
+    // elements of the bin, the elements up to and with it, the sum (bin kBins: not reached).
     auto find_bin = [&](bool by_mass, auto need_of) {
         all_sync();
-        const int per = kBins / nt > 0 ? kBins / nt : 1;  // nt divides kBins
-        u64 v[8], n[8], sv = 0, sn = 0;
-        for (int i = 0; i < per; ++i) {
-            const int b = tid * per + i;
-            u64 w = 0, c = 0;
-            for (int r = 0; r < C; ++r) {
-                c += remote(s.cnt, r)[b];
-                if (by_mass)
-                    w += (u64)remote(s.lo, r)[b] + ((u64)remote(s.hi, r)[b] << 32);
-            }
-            n[i] = c;
-            v[i] = by_mass ? w : c;
-            sv += v[i];
-            sn += c;
+        if (C > 1) {
+            if (rank != 0)
+                for (int b = tid; b < kBins; b += nt)
+                    if (s.cnt[b]) {
+                        atomicAdd(remote(&s.cnt[b], 0), s.cnt[b]);
+                        if (by_mass) {
+                            const uint32_t w = s.lo[b], old = atomicAdd(remote(&s.lo[b], 0), w);
+                            const uint32_t up = s.hi[b] + (old + w < old);
+                            if (up) atomicAdd(remote(&s.hi[b], 0), up);
+                        }
+                    }
+            cluster.sync();
         }
-        u64 total, all;
-        u64 at = block_scan(sv, s.red, &total), en = block_scan(sn, s.red2, &all);
-        const u64 need = need_of(total);
-        for (int i = 0; i < per; ++i) {
-            en += n[i];
-            if (at < need && need <= at + v[i]) {
-                s.found[0] = tid * per + i;
-                s.found[1] = need - at;
-                s.found[2] = n[i];
-                s.found[3] = en;
+        if (rank == 0) {
+            const int per = kBins / nt;  // nt divides kBins
+            u64 sv = 0, sn = 0;
+            for (int b = tid * per; b < (tid + 1) * per; ++b) {
+                sv += by_mass ? (u64)s.lo[b] + ((u64)s.hi[b] << 32) : s.cnt[b];
+                sn += s.cnt[b];
             }
-            at += v[i];
+            u64 total, all;
+            u64 at = block_scan(sv, s.red, &total), en = block_scan(sn, s.red2, &all);
+            const u64 need = need_of(total);
+            auto tell = [&](int i, u64 v) {
+                for (int r = 0; r < C; ++r) *remote(&s.found[i], r) = v;
+            };
+            if (tid == 0) {
+                tell(4, total);
+                if (total < need) tell(0, kBins);
+            }
+            for (int b = tid * per; b < (tid + 1) * per; ++b) {
+                const u64 v = by_mass ? (u64)s.lo[b] + ((u64)s.hi[b] << 32) : s.cnt[b];
+                en += s.cnt[b];
+                if (at < need && need <= at + v) {
+                    tell(0, b);
+                    tell(1, need - at);
+                    tell(2, s.cnt[b]);
+                    tell(3, en);
+                }
+                at += v;
+            }
         }
-        all_sync();  // (the bins have been read everywhere)
-        return total;
+        all_sync();
     };
-    // Elements with `take` go to CTA 0's list.
-    auto gather = [&](auto take) {
+    // Elements of bins up to `last` with `take` go to CTA 0's list (as many as it holds).
+    auto gather = [&](int last, auto take) {
         uint32_t* n = remote(&s.n_list, 0);
         u64* list = remote(s.list, 0);
+        // (a bound below the last bin's edge spares most elements the exact test)
+        const float edge = last >= kBins - 1 ? -INFINITY
+                                             : fminf(top - (last + 1) / scale, FLT_MAX) -
+                                                   fabsf(top) * 0x1p-20f - (last + 1) / scale * 0x1p-20f;
         row.each([&](float x, int i) {
-            if (take(x, i)) list[atomicAdd(n, 1u)] = place(x, i);
+            if (x >= edge && bin_of(x) <= last && take(x, i)) {
+                const uint32_t at = atomicAdd(n, 1u);
+                if (at < kList) list[at] = place(x, i);
+            }
         });
         all_sync();
     };
 
     // The cut of the shortest prefix, within what is kept, that reaches need_of(sum) elements or weight.
-    // True: the whole prefix is in CTA 0's list, sorted (n_list elements, some past it), and `total`
-    // is the sum that it is measured by; false: `cut` is set.
+    // True: the whole prefix is in CTA 0's list (n_list elements, some past it), and `total` is the sum
+    // that it is measured by; false: `cut` is set.
     u64 total = 0;
     auto find = [&](bool by_mass, auto need_of) {
-        const float range = by_mass ? 28.f * t_in : 64.f;  // (weights vanish 27.8 t below the maximum)
-        scale = kBins / fmaxf(fminf(top - bot, range), 0x1p-100f);
+        // (weights vanish 27.8 t below the maximum)
+        scale = kBins / fmaxf(fminf(top - bot, by_mass ? 28.f * t_in : 64.f), 0x1p-100f);
+        const bool all = cut == 0;
         row.each([&](float x, int i) {
-            if (place(x, i) < cut) return;
+            if (!all && place(x, i) < cut) return;
             const int b = bin_of(x);
             if (by_mass) add_mass(b, weight(x));
             atomicAdd(&s.cnt[b], 1u);
         });
-        total = find_bin(by_mass, need_of);
+        find_bin(by_mass, need_of);
+        total = s.found[4];
         const int bin = (int)s.found[0];
         if (s.found[3] <= kList) {
-            const u64 kept = cut;
-            gather([&](float x, int i) { return bin_of(x) <= bin && place(x, i) >= kept; });
-            if (rank == 0) sort_list(s.list, (int)s.n_list, true);
+            gather(bin, [&](float x, int i) { return all || place(x, i) >= cut; });
             return true;
         }
         u64 prefix = 0, need = s.found[1];
@@ -448,19 +487,18 @@ __global__ void __launch_bounds__(1024) sample_kernel(const SampleParams p) {
             prefix = prefix << width | (u64)((1 << width) - 1 - (int)s.found[0]);
             need = s.found[1];
         }
-        const u64 kept = cut;
-        gather([&](float x, int i) {
+        gather(bin, [&](float x, int i) {
             const u64 c = place(x, i);
-            return c >= kept && bin_of(x) == bin && (shift == 32 + kIdxBits || (c >> shift) == prefix);
+            return c >= cut && bin_of(x) == bin && (shift == 32 + kIdxBits || (c >> shift) == prefix);
         });
         if (rank == 0) {
             const int n = (int)s.n_list;
             sort_list(s.list, n, true);
             const int per = (n + nt - 1) / nt;
-            u64 sum = 0, all;
+            u64 sum = 0, all_of;
             for (int i = tid * per; i < min(n, (tid + 1) * per); ++i)
                 sum += by_mass ? weight(place_logit(s.list[i])) : 1;
-            u64 at = block_scan(sum, s.red, &all);
+            u64 at = block_scan(sum, s.red, &all_of);
             for (int i = tid * per; i < min(n, (tid + 1) * per); ++i) {
                 const u64 v = by_mass ? weight(place_logit(s.list[i])) : 1;
                 if (at < need && need <= at + v)
@@ -475,66 +513,146 @@ __global__ void __launch_bounds__(1024) sample_kernel(const SampleParams p) {
         cut = s.cut;
         return false;
     };
+    // k elements at least, and hardly more, from the threads' maxima; false if that does not work out
+    auto find_small_k = [&] {
+        scale = kBins / fmaxf(fminf(top - bot, 64.f), 0x1p-100f);
+        if (thread_top > -INFINITY) atomicAdd(&s.cnt[bin_of(thread_top)], 1u);
+        find_bin(false, [&](u64) { return (u64)k; });
+        const int bin = (int)s.found[0];
+        if (bin < kBins - 1) {
+            gather(bin, [](float, int) { return true; });
+            if (*remote(&s.n_list, 0) <= kList) return true;
+            all_sync();
+        }
+        if (rank == 0 && tid == 0) s.n_list = 0;
+        clear_bins();
+        all_sync();
+        return false;
+    };
     bool in_list = false;
-    if (k < V) in_list = find(false, [&](u64) { return (u64)k; });
+    if (k < V) {
+        in_list = k <= kSmallK && find_small_k();
+        if (!in_list) in_list = find(false, [&](u64) { return (u64)k; });
+    }
     if (use_p && !in_list)
         in_list = find(true, [&](u64 sum) { return max((u64)1, part(sum, pf)); });
 
     if (in_list) {  // CTA 0 has all that can be kept
-        if (rank != 0) return;
+        if (rank != 0) {
+            all_sync();  // (its list length may still be read)
+            return;
+        }
         int n = (int)s.n_list;
+        all_sync();
         const bool by_k = k < V;
+        const bool second = cut != 0;  // the list is top-p's, of what top-k kept
+        if (n <= kPairs) {
+            // four lanes an element: its rank and what comes before it in the order
+            const int q = tid & 3;
+            for (int i = tid; i < n; i += nt) s.w[i] = weight(place_logit(s.list[i]));
+            __syncthreads();
+            for (int i0 = 0; i0 < n; i0 += nt / 4) {
+                const int i = i0 + (tid >> 2);
+                const u64 mine = i < n ? s.list[i] : 0;
+                u64 before = 0;
+                int rank_i = 0;
+                for (int j = q; j < n; j += 4)
+                    if (s.list[j] > mine) {
+                        before += s.w[j];
+                        ++rank_i;
+                    }
+#pragma unroll
+                for (int o = 1; o < 4; o *= 2) {
+                    before += __shfl_xor_sync(0xffffffffu, before, o);
+                    rank_i += __shfl_xor_sync(0xffffffffu, rank_i, o);
+                }
+                if (q == 0 && i < n) {
+                    s.list[kPairs + i] = before;
+                    s.list[2 * kPairs + i] = (u64)rank_i;
+                    if (by_k && rank_i == (int)k - 1) s.part_of = before + s.w[i];
+                }
+            }
+            __syncthreads();
+            const u64 target =
+                !use_p ? ~(u64)0 : max((u64)1, part(by_k && !second ? s.part_of : total, pf));
+            for (int i = tid; i < n; i += nt) {
+                const u64 w = s.w[i], before = s.list[kPairs + i], rank_i = s.list[2 * kPairs + i];
+                // (the first always stays: its weight is the largest)
+                s.list[3 * kPairs + i] =
+                    (!by_k || rank_i < (u64)k) && before < target && w >= floor_w ? w : 0;
+            }
+            __syncthreads();
+            for (int i0 = 0; i0 < n; i0 += nt / 4) {  // what is kept at smaller indices, and in all
+                const int i = i0 + (tid >> 2);
+                const int idx = i < n ? place_index(s.list[i]) : 0;
+                u64 before = 0, all = 0;
+                for (int j = q; j < n; j += 4) {
+                    const u64 w = s.list[3 * kPairs + j];
+                    all += w;
+                    if (place_index(s.list[j]) < idx) before += w;
+                }
+#pragma unroll
+                for (int o = 1; o < 4; o *= 2) {
+                    before += __shfl_xor_sync(0xffffffffu, before, o);
+                    all += __shfl_xor_sync(0xffffffffu, all, o);
+                }
+                const u64 draw = part(all, uf);
+                if (q == 0 && i < n && before <= draw && draw < before + s.list[3 * kPairs + i]) {
+                    p.out[m] = idx;
+                    if (p.p_out) p.p_out[m] = (float)s.list[3 * kPairs + i] / (float)all;
+                }
+            }
+            return;
+        }
+        sort_list(s.list, n, true);
         if (by_k) n = min(n, (int)k);
-        const int per = (kList + nt - 1) / nt;
-        u64 w[8], sum = 0, all;
-        const int j0 = tid * per;
-        for (int i = 0; i < per; ++i) {
-            w[i] = j0 + i < n ? weight(place_logit(s.list[j0 + i])) : 0;
-            sum += w[i];
+        const int per = kList / nt, j0 = tid * per;
+        u64 sum = 0, all;
+        for (int i = j0; i < j0 + per; ++i) {
+            const u64 w = i < n ? weight(place_logit(s.list[i])) : 0;
+            s.w[i] = w;
+            sum += w;
         }
         u64 at = block_scan(sum, s.red, &all);
-        const bool second = cut != 0;  // the list is top-p's, of what top-k kept
-        const u64 target = !use_p ? ~(u64)0
-                                  : max((u64)1, part(by_k && !second ? all : total, pf));
-        // kept: a prefix whose weights before it are short of the target, at least floor_w (the first
-        // always is: its weight is the largest)
-        int kept = 0;
-        for (int i = 0; i < per; ++i) {
-            if (j0 + i < n && at < target && (w[i] >= floor_w)) ++kept;
-            at += w[i];
+        const u64 target = !use_p ? ~(u64)0 : max((u64)1, part(by_k && !second ? all : total, pf));
+        u64 kept = 0, n_kept;  // a prefix
+        for (int i = j0; i < j0 + per; ++i) {
+            if (i < n && at < target && s.w[i] >= floor_w) ++kept;
+            at += s.w[i];
         }
-        u64 n_kept;
-        block_scan((u64)kept, s.red2, &n_kept);
+        block_scan(kept, s.red2, &n_kept);
         n = (int)n_kept;
         __syncthreads();
-        // by the index
-        for (int i = tid; i < n; i += nt) {
+        for (int i = tid; i < n; i += nt) {  // by the index
             const u64 c = s.list[i];
             s.list[i] = (u64)place_index(c) << 32 | (c >> kIdxBits);
         }
         __syncthreads();
         sort_list(s.list, n, false);
         sum = 0;
-        for (int i = 0; i < per; ++i) {
-            w[i] = j0 + i < n ? weight(logit_of((uint32_t)s.list[j0 + i])) : 0;
-            sum += w[i];
+        for (int i = j0; i < j0 + per; ++i) {
+            const u64 w = i < n ? weight(logit_of((uint32_t)s.list[i])) : 0;
+            s.w[i] = w;
+            sum += w;
         }
         at = block_scan(sum, s.red, &all);
         const u64 draw = part(all, uf);
-        for (int i = 0; i < per; ++i) {
-            if (at <= draw && draw < at + w[i]) {
-                p.out[m] = (int32_t)(s.list[j0 + i] >> 32);
-                if (p.p_out) p.p_out[m] = (float)w[i] / (float)all;
+        for (int i = j0; i < j0 + per; ++i) {
+            if (at <= draw && draw < at + s.w[i]) {
+                p.out[m] = (int32_t)(s.list[i] >> 32);
+                if (p.p_out) p.p_out[m] = (float)s.w[i] / (float)all;
             }
-            at += w[i];
+            at += s.w[i];
         }
         return;
     }
 
     // ---- the kept weights in the order of the index: a run of chunks per warp ----
     constexpr int kPer = Row<DT>::kPer;
+    const float cut_x = cut ? place_logit(cut) : -INFINITY;
+    const int cut_i = cut ? place_index(cut) : V;
     auto kept_weight = [&](float x, int i) {
-        if (place(x, i) < cut) return (u64)0;
+        if (x < cut_x || (x == cut_x && i > cut_i)) return (u64)0;
         const u64 w = weight(x);
         return w >= floor_w ? w : (u64)0;
     };
