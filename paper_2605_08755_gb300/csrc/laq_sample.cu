@@ -69,45 +69,77 @@ struct SampleSmem {
     };
     u64 list[kList];
     u64 red[kMaxWarps], red2[kMaxWarps];
-    float fred[2][kMaxWarps];
-    float2 ends[kMaxC];          // (max, min) of every CTA of the cluster
+    float fred[kMaxWarps];
+    float ends[kMaxC];           // the largest element, then a bin, of every CTA of the cluster
     u64 sums[kMaxC];             // kept weight of every CTA
     u64 found[5], cut, part_of;
     uint32_t n_list, first;
 };
 
+// 16 bytes of logits: kPer of them, NaN taken as -inf.
 template <int DT>
-struct Logits;  // 16 bytes of logits as floats; NaN as -inf, -0 as 0
+struct Logits;
 template <>
 struct Logits<LAQ_F32> {
     static constexpr int kPer = 4, kSize = 4;
+    static constexpr uint32_t kLeast = 0xff800000u;  // -inf
+    static __device__ __forceinline__ uint32_t clean(uint32_t w) {
+        return __float_as_uint(fmaxf(__uint_as_float(w), -INFINITY));
+    }
     static __device__ __forceinline__ void unpack(const uint4& u, float (&x)[kPer]) {
         x[0] = __uint_as_float(u.x); x[1] = __uint_as_float(u.y);
         x[2] = __uint_as_float(u.z); x[3] = __uint_as_float(u.w);
     }
-    static __device__ __forceinline__ uint32_t raw(const void* p, int64_t i) {
-        return static_cast<const uint32_t*>(p)[i];
+    static __device__ __forceinline__ uint32_t word(const void* p, int i, int n) {  // elements i ..
+        return i < n ? static_cast<const uint32_t*>(p)[i] : kLeast;
+    }
+    static __device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) {
+        return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b)));
+    }
+    static __device__ __forceinline__ float largest(uint32_t w) { return __uint_as_float(w); }
+    static __device__ __forceinline__ float at(const void* p, int i) {
+        return fmaxf(static_cast<const float*>(p)[i], -INFINITY);
     }
 };
 template <bool BF>
 struct Logits16 {
     static constexpr int kPer = 8, kSize = 2;
+    static constexpr uint32_t kLeast = BF ? 0xff80ff80u : 0xfc00fc00u;
+    static __device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) {  // (a NaN loses)
+        if (BF) {
+            const __nv_bfloat162 m = __hmax2(*reinterpret_cast<const __nv_bfloat162*>(&a),
+                                             *reinterpret_cast<const __nv_bfloat162*>(&b));
+            return *reinterpret_cast<const uint32_t*>(&m);
+        }
+        const __half2 m = __hmax2(*reinterpret_cast<const __half2*>(&a),
+                                  *reinterpret_cast<const __half2*>(&b));
+        return *reinterpret_cast<const uint32_t*>(&m);
+    }
+    static __device__ __forceinline__ uint32_t clean(uint32_t w) { return larger(w, kLeast); }
+    static __device__ __forceinline__ float2 two(uint32_t w) {
+        if (BF) return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+        return __half22float2(*reinterpret_cast<const __half2*>(&w));
+    }
     static __device__ __forceinline__ void unpack(const uint4& u, float (&x)[kPer]) {
         const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            if (BF) {
-                x[2 * i] = __uint_as_float(w[i] << 16);
-                x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-            } else {
-                const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
-                x[2 * i] = f.x;
-                x[2 * i + 1] = f.y;
-            }
+            const float2 f = two(w[i]);
+            x[2 * i] = f.x;
+            x[2 * i + 1] = f.y;
         }
     }
-    static __device__ __forceinline__ uint32_t raw(const void* p, int64_t i) {
-        return static_cast<const uint16_t*>(p)[i];
+    static __device__ __forceinline__ uint32_t word(const void* p, int i, int n) {
+        const uint16_t* h = static_cast<const uint16_t*>(p);
+        const uint32_t lo = i < n ? h[i] : kLeast & 0xffffu;
+        return lo | (i + 1 < n ? (uint32_t)h[i + 1] << 16 : kLeast & 0xffff0000u);
+    }
+    static __device__ __forceinline__ float largest(uint32_t w) {
+        const float2 f = two(w);
+        return fmaxf(f.x, f.y);
+    }
+    static __device__ __forceinline__ float at(const void* p, int i) {
+        return fmaxf(two(static_cast<const uint16_t*>(p)[i]).x, -INFINITY);
     }
 };
 template <>
@@ -115,11 +147,9 @@ struct Logits<LAQ_F16> : Logits16<false> {};
 template <>
 struct Logits<LAQ_BF16> : Logits16<true> {};
 
-__device__ __forceinline__ float clean(float x) { return fmaxf(x, -INFINITY) + 0.f; }
-
 // order-preserving key of a logit, and back
 __device__ __forceinline__ uint32_t key_of(float x) {
-    const uint32_t b = __float_as_uint(x);
+    const uint32_t b = __float_as_uint(x + 0.f);  // (the two zeros are one value)
     return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
 }
 __device__ __forceinline__ float logit_of(uint32_t key) {
@@ -127,7 +157,7 @@ __device__ __forceinline__ float logit_of(uint32_t key) {
 }
 // place in the order: larger first
 __device__ __forceinline__ u64 place(float x, int idx) {
-    return (u64)key_of(x) << kIdxBits | (u64)((1 << kIdxBits) - 1 - idx);
+    return (u64)key_of(x) << kIdxBits | (~(uint32_t)idx & ((1u << kIdxBits) - 1));
 }
 __device__ __forceinline__ float place_logit(u64 c) { return logit_of((uint32_t)(c >> kIdxBits)); }
 __device__ __forceinline__ int place_index(u64 c) {
@@ -141,23 +171,35 @@ __device__ __forceinline__ u64 part(u64 mass, uint32_t f) {
 // A row's weights.
 struct Weights {
     float top, t, r;
-    bool plain;  // t so large or small that its reciprocal is not a normal number
+    bool fast;  // the reciprocal of t is a normal number and the maximum a finite one
     __device__ Weights(float top_, float t_) : top(top_), t(t_), r(1.f / t_) {
-        plain = !(t > 0x1p-100f && t < 0x1p100f);
+        fast = t > 0x1p-100f && t < 0x1p100f && top < INFINITY;
+    }
+    // The weight of a fast row as high * 2^20 + low, low < 2^20: floor(e * 2^20) and floor of what is left
+    // of it times 2^20, each as the low bits of a float around 2^23 (with kBias above them).
+    static constexpr uint32_t kBias = 0x4b000000u;
+    __device__ __forceinline__ void parts(float x, uint32_t& high, uint32_t& low) const {
+        const float d = x - top;
+        float q = fmaxf(d * r, -64.f);  // (past -28 the weight is 0: the bound keeps -inf apart from +inf)
+        q = fmaf(fmaf(-q, t, d), r, q);
+        const float e = expf(q);
+        const float h = __fmaf_rd(e, 0x1p20f, 0x1p23f);
+        const float left = fmaf(e, 0x1p20f, 0x1p23f - h);  // (exact: h - 2^23 is floor(e * 2^20))
+        high = __float_as_uint(h);
+        low = __float_as_uint(__fmaf_rd(left, 0x1p20f, 0x1p23f));
     }
     __device__ __forceinline__ u64 operator()(float x) const {
-        const float d = x - top;
-        float q;
-        if (plain) {
-            q = x == -INFINITY ? -INFINITY : d / t;
-        } else {
-            q = fmaxf(d * r, -64.f);  // (past -28 the weight is 0: the bound keeps -inf apart from +inf)
-            q = fmaf(fmaf(-q, t, d), r, q);
+        if (fast) {
+            uint32_t h, l;
+            parts(x, h, l);
+            return ((u64)(h - kBias) << 20) + (l - kBias);
         }
-        // floor(e * 2^40) of e = significand * 2^(exponent - 23), e <= 1 (a NaN, of infinite t, is 0)
-        const uint32_t e = __float_as_uint(expf(q));
-        const u64 w = (u64)((e & 0x7fffffu) | 0x800000u) << 17 >> min(127u - min(e >> 23, 127u), 63u);
-        return x == top ? (u64)1 << 40 : e < 0x7f800000u ? w : 0;
+        return slow(x);
+    }
+    __device__ __noinline__ u64 slow(float x) const {
+        if (x == top) return (u64)1 << 40;
+        if (x == -INFINITY || top == INFINITY) return 0;
+        return (u64)(expf((x - top) / t) * 0x1p40f);
     }
 };
 
@@ -168,31 +210,35 @@ struct Row {
     int n, i0;            // its elements, the first one's index in the row
     bool aligned;
 
+    // chunk c of 16 bytes; past the slice's end: -inf (of no weight, so that it makes no difference where
+    // such elements are counted or listed)
     __device__ __forceinline__ uint4 raw(int c) const {
-        if (aligned) {
-            if (kPer * (c + 1) <= n) return *reinterpret_cast<const uint4*>(src + 16 * (size_t)c);
+        uint4 u;
+        if (aligned && kPer * (c + 1) <= n) {
+            u = *reinterpret_cast<const uint4*>(src + 16 * (size_t)c);
+        } else {
+            constexpr int kWord = kPer / 4;
+            u.x = Logits<DT>::word(src, kPer * c, n);
+            u.y = Logits<DT>::word(src, kPer * c + kWord, n);
+            u.z = Logits<DT>::word(src, kPer * c + 2 * kWord, n);
+            u.w = Logits<DT>::word(src, kPer * c + 3 * kWord, n);
         }
-        uint32_t e[4] = {0u, 0u, 0u, 0u};
-#pragma unroll
-        for (int k = 0; k < kPer; ++k) {
-            const int i = kPer * c + k;
-            const uint32_t v = i < n ? Logits<DT>::raw(src, i) : 0u;
-            if (kPer == 4) e[k] = v;
-            else e[k >> 1] |= v << (16 * (k & 1));
-        }
-        return make_uint4(e[0], e[1], e[2], e[3]);
+        u.x = Logits<DT>::clean(u.x);
+        u.y = Logits<DT>::clean(u.y);
+        u.z = Logits<DT>::clean(u.z);
+        u.w = Logits<DT>::clean(u.w);
+        return u;
     }
-    // f(x, index in the row) of the calling thread's elements, chunks of 16 bytes strided over the CTA
+    // f(x, index in the row) of the calling thread's elements, chunks strided over the CTA
     template <typename F>
     __device__ __forceinline__ void each(F f) const {
         const int chunks = (n + kPer - 1) / kPer;
+#pragma unroll 1
         for (int c = threadIdx.x; c < chunks; c += blockDim.x) {
             float x[kPer];
             Logits<DT>::unpack(raw(c), x);
-            const int m = n - kPer * c;
 #pragma unroll
-            for (int k = 0; k < kPer; ++k)
-                if (k < m) f(clean(x[k]), i0 + kPer * c + k);
+            for (int k = 0; k < kPer; ++k) f(x[k], i0 + kPer * c + k);
         }
     }
 };
@@ -268,11 +314,13 @@ __global__ void __launch_bounds__(1024) sample_kernel(const SampleParams p) {
               ((size_t)m * p.row_stride + row.i0) * Logits<DT>::kSize;
     row.aligned = ((uintptr_t)row.src & 15u) == 0;
 
-    // ---- one pass over the row: the slice into shared memory, its largest and least element ----
-    float top = -INFINITY, bot = INFINITY;
+    // ---- one pass over the row: the slice into shared memory, and its largest element ----
+    float top;
     {
         constexpr int kPer = Row<DT>::kPer, kDeep = 4;
+        uint32_t most = Logits<DT>::kLeast;
         const int chunks = (row.n + kPer - 1) / kPer;
+#pragma unroll 1
         for (int c0 = tid; c0 < chunks; c0 += kDeep * nt) {
             uint4 u[kDeep];
 #pragma unroll
@@ -283,59 +331,42 @@ __global__ void __launch_bounds__(1024) sample_kernel(const SampleParams p) {
                 const int c = c0 + a * nt;
                 if (c >= chunks) break;
                 if (p.resident) *reinterpret_cast<uint4*>(slice + 16 * (size_t)c) = u[a];
-                float x[kPer];
-                Logits<DT>::unpack(u[a], x);
-#pragma unroll
-                for (int k = 0; k < kPer; ++k)
-                    if (kPer * c + k < row.n) {
-                        const float y = clean(x[k]);
-                        top = fmaxf(top, y);
-                        if (y > -INFINITY) bot = fminf(bot, y);
-                    }
+                most = Logits<DT>::larger(most, Logits<DT>::larger(Logits<DT>::larger(u[a].x, u[a].y),
+                                                                   Logits<DT>::larger(u[a].z, u[a].w)));
             }
         }
+        top = Logits<DT>::largest(most);
         if (p.resident) {
             row.src = slice;
             row.aligned = true;
+            row.n = chunks * kPer;  // (the last chunk's end is -inf in the copy)
         }
     }
     const float thread_top = top;
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-        bot = fminf(bot, __shfl_xor_sync(0xffffffffu, bot, o));
-    }
-    if (lane == 0) {
-        s.fred[0][warp] = top;
-        s.fred[1][warp] = bot;
-    }
+    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    if (lane == 0) s.fred[warp] = top;
     if (tid == 0) {
         s.n_list = 0;
         s.first = 0xffffffffu;
     }
     auto clear_bins = [&] {
+#pragma unroll 1
         for (int i = tid; i < kBins; i += nt) s.cnt[i] = s.lo[i] = s.hi[i] = 0;
     };
     clear_bins();
     __syncthreads();
-    if (warp == 0) {
-        top = lane < nt / 32 ? s.fred[0][lane] : -INFINITY;
-        bot = lane < nt / 32 ? s.fred[1][lane] : INFINITY;
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) {
-            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-            bot = fminf(bot, __shfl_xor_sync(0xffffffffu, bot, o));
-        }
-    }
     // (every CTA of the cluster has to have started before its shared memory is written)
     if (C > 1) asm volatile("barrier.cluster.wait.aligned;\n" ::: "memory");
-    if (warp == 0 && lane < C) remote(&s.ends[0], lane)[rank] = make_float2(top, bot);
-    all_sync();
-    top = -INFINITY, bot = INFINITY;
-    for (int r = 0; r < C; ++r) {
-        top = fmaxf(top, s.ends[r].x);
-        bot = fminf(bot, s.ends[r].y);
+    if (warp == 0) {
+        top = lane < nt / 32 ? s.fred[lane] : -INFINITY;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        if (lane < C) remote(&s.ends[0], lane)[rank] = top;
     }
+    all_sync();
+    top = s.ends[0];
+    for (int r = 1; r < C; ++r) top = fmaxf(top, s.ends[r]);
     if (top == -INFINITY) {  // (all CTAs of the cluster agree)
         if (rank == 0 && tid == 0) {
             p.out[m] = 0;
@@ -429,21 +460,71 @@ __global__ void __launch_bounds__(1024) sample_kernel(const SampleParams p) {
         }
         all_sync();
     };
-    // Elements of bins up to `last` with `take` go to CTA 0's list (as many as it holds).
-    auto gather = [&](int last, auto take) {
-        uint32_t* n = remote(&s.n_list, 0);
-        u64* list = remote(s.list, 0);
-        // (a bound below the last bin's edge spares most elements the exact test)
-        const float edge = last >= kBins - 1 ? -INFINITY
-                                             : fminf(top - (last + 1) / scale, FLT_MAX) -
-                                                   fabsf(top) * 0x1p-20f - (last + 1) / scale * 0x1p-20f;
+    // Elements of bins first .. last with `take` go to CTA 0's list (as many as it holds), the other CTAs'
+    // by way of their own (an atomic a element across the cluster stalls its warp for 1500 cycles).
+    auto gather = [&](int first, int last, auto take) {
+        // (bounds outside the bins' edges spare most elements the exact test)
+        const float slack = fabsf(top) * 0x1p-20f;
+        auto edge = [&](int b, float e) { return top - b / scale * (1.f - e) + e * slack; };
+        const float lo = last >= kBins - 1 || !(scale > 0.f) ? -INFINITY : edge(last + 1, -0x1p-18f) - slack;
+        const float hi = first <= 1 || !(scale > 0.f) ? INFINITY : edge(first, 0x1p-18f) + slack;
         row.each([&](float x, int i) {
-            if (x >= edge && bin_of(x) <= last && take(x, i)) {
-                const uint32_t at = atomicAdd(n, 1u);
-                if (at < kList) list[at] = place(x, i);
+            if (x >= lo && x <= hi) {
+                const int b = bin_of(x);
+                if (b >= first && b <= last && take(x, i)) {
+                    const uint32_t at = atomicAdd(&s.n_list, 1u);
+                    if (at < kList) s.list[at] = place(x, i);
+                }
             }
         });
-        all_sync();
+        if (C > 1) {
+            if (rank != 0) {
+                __syncthreads();
+                const uint32_t n = s.n_list;
+                if (tid == 0 && n) s.first = atomicAdd(remote(&s.n_list, 0), n);
+                __syncthreads();
+                u64* list = remote(s.list, 0);
+                for (uint32_t i = tid; i < min(n, (uint32_t)kList); i += nt)
+                    if (s.first + i < kList) list[s.first + i] = s.list[i];
+                if (tid == 0) s.n_list = 0;
+            }
+            cluster.sync();
+        } else {
+            __syncthreads();
+        }
+    };
+    // Weights and counts of the elements with `take` into the bins.
+    auto count_mass = [&](auto take) {
+        if (weight.fast) {
+            // in two parts of 20 bits, added without waiting; a bin of 4096 elements could wrap
+            row.each([&](float x, int i) {
+                uint32_t h, l;
+                weight.parts(x, h, l);
+                const int b = take(x, i);
+                if (b < 0) return;
+                atomicAdd(&s.cnt[b], 1u);
+                atomicAdd(&s.lo[b], l - Weights::kBias);
+                atomicAdd(&s.hi[b], h - Weights::kBias);
+            });
+            __syncthreads();
+            bool wraps = false;
+#pragma unroll 1
+            for (int b = tid; b < kBins; b += nt) {
+                const u64 v = ((u64)s.hi[b] << 20) + s.lo[b];
+                s.lo[b] = (uint32_t)v;
+                s.hi[b] = (uint32_t)(v >> 32);
+                wraps |= s.cnt[b] > 4095;
+            }
+            if (!__syncthreads_or(wraps)) return;
+            clear_bins();
+            __syncthreads();
+        }
+        row.each([&](float x, int i) {
+            const int b = take(x, i);
+            if (b < 0) return;
+            add_mass(b, weight(x));
+            atomicAdd(&s.cnt[b], 1u);
+        });
     };
 
     // The cut of the shortest prefix, within what is kept, that reaches need_of(sum) elements or weight.
@@ -452,19 +533,17 @@ __global__ void __launch_bounds__(1024) sample_kernel(const SampleParams p) {
     u64 total = 0;
     auto find = [&](bool by_mass, auto need_of) {
         // (weights vanish 27.8 t below the maximum)
-        scale = kBins / fmaxf(fminf(top - bot, by_mass ? 28.f * t_in : 64.f), 0x1p-100f);
+        scale = kBins / (by_mass ? 28.f * t_in : 64.f);
         const bool all = cut == 0;
-        row.each([&](float x, int i) {
-            if (!all && place(x, i) < cut) return;
-            const int b = bin_of(x);
-            if (by_mass) add_mass(b, weight(x));
-            atomicAdd(&s.cnt[b], 1u);
-        });
+        if (by_mass)
+            count_mass([&](float x, int i) { return all || place(x, i) >= cut ? bin_of(x) : -1; });
+        else
+            row.each([&](float x, int i) { atomicAdd(&s.cnt[bin_of(x)], 1u); });
         find_bin(by_mass, need_of);
         total = s.found[4];
         const int bin = (int)s.found[0];
         if (s.found[3] <= kList) {
-            gather(bin, [&](float x, int i) { return all || place(x, i) >= cut; });
+            gather(0, bin, [&](float x, int i) { return all || place(x, i) >= cut; });
             return true;
         }
         u64 prefix = 0, need = s.found[1];
@@ -475,21 +554,26 @@ __global__ void __launch_bounds__(1024) sample_kernel(const SampleParams p) {
             __syncthreads();
             clear_bins();
             __syncthreads();
-            row.each([&](float x, int i) {
+            auto digit = [&](float x, int i) {
                 const u64 c = place(x, i);
-                if (c < cut || bin_of(x) != bin || (c >> (shift + width)) != prefix) return;
+                if (c < cut || bin_of(x) != bin || (c >> (shift + width)) != prefix) return -1;
                 // (bins ascend as the order does: the largest place first)
-                const int b = (1 << width) - 1 - (int)((c >> shift) & ((1u << width) - 1));
-                if (by_mass) add_mass(b, weight(x));
-                atomicAdd(&s.cnt[b], 1u);
-            });
+                return (1 << width) - 1 - (int)((c >> shift) & ((1u << width) - 1));
+            };
+            if (by_mass)
+                count_mass(digit);
+            else
+                row.each([&](float x, int i) {
+                    const int b = digit(x, i);
+                    if (b >= 0) atomicAdd(&s.cnt[b], 1u);
+                });
             find_bin(by_mass, [&](u64) { return need; });
             prefix = prefix << width | (u64)((1 << width) - 1 - (int)s.found[0]);
             need = s.found[1];
         }
-        gather(bin, [&](float x, int i) {
+        gather(bin, bin, [&](float x, int i) {
             const u64 c = place(x, i);
-            return c >= cut && bin_of(x) == bin && (shift == 32 + kIdxBits || (c >> shift) == prefix);
+            return c >= cut && (shift == 32 + kIdxBits || (c >> shift) == prefix);
         });
         if (rank == 0) {
             const int n = (int)s.n_list;
@@ -515,12 +599,12 @@ __global__ void __launch_bounds__(1024) sample_kernel(const SampleParams p) {
     };
     // k elements at least, and hardly more, from the threads' maxima; false if that does not work out
     auto find_small_k = [&] {
-        scale = kBins / fmaxf(fminf(top - bot, 64.f), 0x1p-100f);
+        scale = kBins / 64.f;
         if (thread_top > -INFINITY) atomicAdd(&s.cnt[bin_of(thread_top)], 1u);
         find_bin(false, [&](u64) { return (u64)k; });
         const int bin = (int)s.found[0];
         if (bin < kBins - 1) {
-            gather(bin, [](float, int) { return true; });
+            gather(0, bin, [](float, int) { return true; });
             if (*remote(&s.n_list, 0) <= kList) return true;
             all_sync();
         }
@@ -652,19 +736,35 @@ __global__ void __launch_bounds__(1024) sample_kernel(const SampleParams p) {
     const float cut_x = cut ? place_logit(cut) : -INFINITY;
     const int cut_i = cut ? place_index(cut) : V;
     auto kept_weight = [&](float x, int i) {
-        if (x < cut_x || (x == cut_x && i > cut_i)) return (u64)0;
+        if (x < cut_x || (x == cut_x && i > cut_i) || i >= V) return (u64)0;
         const u64 w = weight(x);
         return w >= floor_w ? w : (u64)0;
     };
     const int chunks = (row.n + kPer - 1) / kPer, warps = nt >> 5;
     const int run = ((chunks + warps - 1) / warps + 31) / 32 * 32;  // chunks of a warp
     u64 sum = 0;
+#pragma unroll 1
     for (int c = warp * run + lane; c < min(chunks, (warp + 1) * run); c += 32) {
         float x[kPer];
         Logits<DT>::unpack(row.raw(c), x);
+        if (weight.fast && floor_w == 0) {
+            uint32_t high = 0, low = 0, n = 0;
 #pragma unroll
-        for (int e = 0; e < kPer; ++e)
-            if (kPer * c + e < row.n) sum += kept_weight(clean(x[e]), row.i0 + kPer * c + e);
+            for (int e = 0; e < kPer; ++e) {
+                uint32_t h, l;
+                weight.parts(x[e], h, l);
+                const bool on = x[e] > cut_x || (x[e] == cut_x && row.i0 + kPer * c + e <= cut_i);
+                high += on ? h : 0u;
+                low += on ? l : 0u;
+                n += on;
+            }
+            sum += ((u64)(high - n * Weights::kBias) << 20) + (low - n * Weights::kBias);
+        } else {
+#pragma unroll 1
+            for (int e = 0; e < kPer; ++e)
+                sum += kept_weight(Logits<DT>::at(row.src, min(kPer * c + e, row.n - 1)),
+                                   kPer * c + e < row.n ? row.i0 + kPer * c + e : V);
+        }
     }
     u64 mine;
     block_scan(sum, s.red, &mine);  // (red: the warps' sums)
@@ -683,14 +783,7 @@ __global__ void __launch_bounds__(1024) sample_kernel(const SampleParams p) {
     const int e0 = w0 * run * kPer, e1 = min(row.n, (w0 + 1) * run * kPer);
     const int per = (e1 - e0 + nt - 1) / nt;
     sum = 0;
-    auto at_index = [&](int i) {
-        float x;
-        const uint32_t v = Logits<DT>::raw(row.src, i);
-        if (DT == LAQ_F32) x = __uint_as_float(v);
-        else if (DT == LAQ_F16) x = __half2float(__ushort_as_half((unsigned short)v));
-        else x = __uint_as_float(v << 16);
-        return kept_weight(clean(x), row.i0 + i);
-    };
+    auto at_index = [&](int i) { return kept_weight(Logits<DT>::at(row.src, i), row.i0 + i); };
     for (int i = e0 + tid * per; i < min(e1, e0 + (tid + 1) * per); ++i) sum += at_index(i);
     u64 run_sum;
     before += block_scan(sum, s.red2, &run_sum);
