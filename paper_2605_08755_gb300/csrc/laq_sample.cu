@@ -265,18 +265,55 @@ __device__ __forceinline__ u64 block_scan(u64 v, u64* red, u64* total) {
     return before + inc - v;
 }
 
-// Sort the first n of list (padded to a power of two), descending or ascending.
+// Sort the first n of list (padded to a power of two), descending or ascending: a bitonic network, with
+// an element a thread in a register and the exchanges within a warp by shuffles (a barrier for each of
+// them made a sort of 512 cost 13,000 cycles), or in place where there are more elements than threads.
 __device__ __noinline__ void sort_list(u64* list, int n, bool descending) {
+    const int tid = threadIdx.x, nt = blockDim.x;
     int N = 32;
     while (N < n) N *= 2;
-    for (int i = n + threadIdx.x; i < N; i += blockDim.x) list[i] = descending ? 0 : ~(u64)0;
+    const u64 pad = descending ? 0 : ~(u64)0;
+    if (N <= nt) {
+        u64 v = tid < n ? list[tid] : pad;
+        if (tid < N) {  // (whole warps)
+#pragma unroll 1
+            for (int k = 2; k <= 32; k *= 2)
+#pragma unroll 1
+                for (int j = k / 2; j > 0; j /= 2) {
+                    const u64 y = __shfl_xor_sync(0xffffffffu, v, j);
+                    // the lower of the two keeps the smaller where its run ascends
+                    const bool small = (((tid & k) == 0) != descending) == ((tid & j) == 0);
+                    if ((v > y) == small) v = y;
+                }
+        }
+#pragma unroll 1
+        for (int k = 64; k <= N; k *= 2)
+#pragma unroll 1
+            for (int j = k / 2; j > 0; j /= 2) {
+                if (j >= 32) {
+                    __syncthreads();
+                    if (tid < N) list[tid] = v;
+                    __syncthreads();
+                }
+                if (tid < N) {
+                    const u64 y = j >= 32 ? list[tid ^ j] : __shfl_xor_sync(0xffffffffu, v, j);
+                    const bool small = (((tid & k) == 0) != descending) == ((tid & j) == 0);
+                    if ((v > y) == small) v = y;
+                }
+            }
+        __syncthreads();
+        if (tid < N) list[tid] = v;
+        __syncthreads();
+        return;
+    }
+    for (int i = n + tid; i < N; i += nt) list[i] = pad;
 #pragma unroll 1
     for (int k = 2; k <= N; k *= 2)
 #pragma unroll 1
         for (int j = k / 2; j > 0; j /= 2) {
             __syncthreads();
 #pragma unroll 1
-            for (int i = threadIdx.x; i < N / 2; i += blockDim.x) {
+            for (int i = tid; i < N / 2; i += nt) {
                 const int a = 2 * i - (i & (j - 1)), b = a + j;
                 const u64 x = list[a], y = list[b];
                 const bool up = ((a & k) == 0) != descending;  // this run ascends
@@ -468,15 +505,25 @@ __global__ void __launch_bounds__(1024) sample_kernel(const SampleParams p) {
         auto edge = [&](int b, float e) { return top - b / scale * (1.f - e) + e * slack; };
         const float lo = last >= kBins - 1 || !(scale > 0.f) ? -INFINITY : edge(last + 1, -0x1p-18f) - slack;
         const float hi = first <= 1 || !(scale > 0.f) ? INFINITY : edge(first, 0x1p-18f) + slack;
-        row.each([&](float x, int i) {
-            if (x >= lo && x <= hi) {
-                const int b = bin_of(x);
-                if (b >= first && b <= last && take(x, i)) {
-                    const uint32_t at = atomicAdd(&s.n_list, 1u);
-                    if (at < kList) s.list[at] = place(x, i);
+        constexpr int kPer = Row<DT>::kPer;
+        const int chunks = (row.n + kPer - 1) / kPer;
+#pragma unroll 2
+        for (int c = tid; c < chunks; c += nt) {
+            const uint4 u = row.raw(c);
+            typedef Logits<DT> L;
+            if (L::largest(L::larger(L::larger(u.x, u.y), L::larger(u.z, u.w))) < lo) continue;
+            float x[kPer];
+            L::unpack(u, x);
+#pragma unroll
+            for (int k = 0; k < kPer; ++k)
+                if (x[k] >= lo && x[k] <= hi) {
+                    const int b = bin_of(x[k]), i = row.i0 + kPer * c + k;
+                    if (b >= first && b <= last && take(x[k], i)) {
+                        const uint32_t at = atomicAdd(&s.n_list, 1u);
+                        if (at < kList) s.list[at] = place(x[k], i);
+                    }
                 }
-            }
-        });
+        }
         if (C > 1) {
             if (rank != 0) {
                 __syncthreads();
@@ -597,14 +644,29 @@ __global__ void __launch_bounds__(1024) sample_kernel(const SampleParams p) {
         cut = s.cut;
         return false;
     };
-    // k elements at least, and hardly more, from the threads' maxima; false if that does not work out
+    // k elements at least, and hardly more: each CTA's bin up to which the maxima of k / C of its threads
+    // lie, and of these bins the last.  False if that does not work out.
     auto find_small_k = [&] {
         scale = kBins / 64.f;
         if (thread_top > -INFINITY) atomicAdd(&s.cnt[bin_of(thread_top)], 1u);
-        find_bin(false, [&](u64) { return (u64)k; });
-        const int bin = (int)s.found[0];
+        if (tid == 0) s.found[0] = kBins;
+        __syncthreads();
+        const u64 need = (u64)(k + C - 1) / C;
+        const int per = kBins / nt;
+        u64 sum = 0, all;
+        for (int b = tid * per; b < (tid + 1) * per; ++b) sum += s.cnt[b];
+        u64 at = block_scan(sum, s.red, &all);
+        for (int b = tid * per; b < (tid + 1) * per; ++b) {
+            if (at < need && need <= at + s.cnt[b]) s.found[0] = b;
+            at += s.cnt[b];
+        }
+        __syncthreads();
+        if (tid < C) remote(s.ends, tid)[rank] = (float)s.found[0];
+        all_sync();
+        float bin = s.ends[0];
+        for (int r = 1; r < C; ++r) bin = fmaxf(bin, s.ends[r]);
         if (bin < kBins - 1) {
-            gather(0, bin, [](float, int) { return true; });
+            gather(0, (int)bin, [](float, int) { return true; });
             if (*remote(&s.n_list, 0) <= kList) return true;
             all_sync();
         }
