@@ -60,7 +60,7 @@ struct SampleParams {
     int V, C, slice, resident;  // slice: elements per CTA (a multiple of 8); resident: kept in smem
 };
 
-struct SampleSmem {
+struct alignas(16) SampleSmem {
     union {
         struct {
             uint32_t cnt[kBins], lo[kBins], hi[kBins];
@@ -72,8 +72,8 @@ struct SampleSmem {
     float fred[kMaxWarps];
     float ends[kMaxC];           // the largest element, then a bin, of every CTA of the cluster
     u64 sums[kMaxC];             // kept weight of every CTA
-    u64 found[5], cut, part_of;
-    uint32_t n_list, first;
+    u64 found[5], cut, part_of, need;
+    uint32_t n_list, first, counts[kMaxC];
 };
 
 // 16 bytes of logits: kPer of them, NaN taken as -inf.
@@ -188,15 +188,9 @@ struct Weights {
         high = __float_as_uint(h);
         low = __float_as_uint(__fmaf_rd(left, 0x1p20f, 0x1p23f));
     }
-    __device__ __forceinline__ u64 operator()(float x) const {
-        if (fast) {
-            uint32_t h, l;
-            parts(x, h, l);
-            return ((u64)(h - kBias) << 20) + (l - kBias);
-        }
-        return slow(x);
-    }
-    __device__ __noinline__ u64 slow(float x) const {
+    __device__ __forceinline__ u64 operator()(float x) const { return weight_of(x, top, t); }
+    // (one copy of it, for the short loops: code that runs once is paid for by the instruction)
+    static __device__ __noinline__ u64 weight_of(float x, float top, float t) {
         if (x == top) return (u64)1 << 40;
         if (x == -INFINITY || top == INFINITY) return 0;
         return (u64)(expf((x - top) / t) * 0x1p40f);
@@ -252,7 +246,7 @@ __device__ __forceinline__ u64 warp_scan(u64 v) {  // inclusive
     return v;
 }
 // exclusive prefix over the CTA and the total (two barriers)
-__device__ __forceinline__ u64 block_scan(u64 v, u64* red, u64* total) {
+__device__ __noinline__ u64 block_scan(u64 v, u64* red, u64* total) {
     const int warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
     const u64 inc = warp_scan(v);
     __syncthreads();
@@ -344,6 +338,10 @@ __global__ void __launch_bounds__(1024) sample_kernel(const SampleParams p) {
     };
     auto remote = [&](auto* ptr, int r) { return C > 1 ? cluster.map_shared_rank(ptr, r) : ptr; };
     pdl_wait();
+    // (the row's settings, asked for before its logits)
+    const float t_in = p.temperature ? p.temperature[m] : 1.f, u = p.u[m];
+    const float fp = p.top_p ? p.top_p[m] : 1.f, fm = p.min_p ? p.min_p[m] : 0.f;
+    const int k_in = p.top_k ? p.top_k[m] : 0;
     Row<DT> row;
     row.i0 = min(V, rank * p.slice);
     row.n = min(V - row.i0, p.slice);
@@ -413,9 +411,7 @@ __global__ void __launch_bounds__(1024) sample_kernel(const SampleParams p) {
     }
 
     // ---- the row's settings ----
-    const float t_in = p.temperature ? p.temperature[m] : 1.f;
-    int64_t k = p.top_k ? p.top_k[m] : 0;
-    if (k <= 0 || k > V) k = V;
+    const int k = k_in <= 0 || k_in > V ? V : k_in;
     if (!(t_in > 0.f) || (k == 1 && V > 1) || V == 1) {  // the first maximum
         uint32_t first = 0xffffffffu;
         row.each([&](float x, int i) {
@@ -431,11 +427,9 @@ __global__ void __launch_bounds__(1024) sample_kernel(const SampleParams p) {
         return;
     }
     const Weights weight(top, t_in);
-    const float fp = p.top_p ? p.top_p[m] : 1.f, fm = p.min_p ? p.min_p[m] : 0.f;
     const bool use_p = fp < 1.f;
     const uint32_t pf = use_p ? (uint32_t)(fmaxf(fp, 0.f) * 0x1p24f) : 0u;
     const u64 floor_w = fm > 0.f ? (u64)(fminf(fm, 1.f) * 0x1p40f) : 0;
-    const float u = p.u[m];
     const uint32_t uf = u > 0.f ? min((uint32_t)(fminf(u, 1.f) * 0x1p24f), 0xffffffu) : 0u;
 
     u64 cut = 0;        // what is kept: elements whose place is at least this
@@ -448,106 +442,27 @@ __global__ void __launch_bounds__(1024) sample_kernel(const SampleParams p) {
         const uint32_t up = (uint32_t)(w >> 32) + (old + wl < old);
         if (up) atomicAdd(&s.hi[b], up);
     };
-    // The cluster's bins, added up in CTA 0: prefix sums of counts or weights, and the bin where they
-    // reach need_of(sum over all bins).  found, in all CTAs: bin, what is left of the need in it, the
-    // elements of the bin, the elements up to and with it, the sum (bin kBins: not reached).
-    auto find_bin = [&](bool by_mass, auto need_of) {
-        all_sync();
-        if (C > 1) {
-            if (rank != 0)
-                for (int b = tid; b < kBins; b += nt)
-                    if (s.cnt[b]) {
-                        atomicAdd(remote(&s.cnt[b], 0), s.cnt[b]);
-                        if (by_mass) {
-                            const uint32_t w = s.lo[b], old = atomicAdd(remote(&s.lo[b], 0), w);
-                            const uint32_t up = s.hi[b] + (old + w < old);
-                            if (up) atomicAdd(remote(&s.hi[b], 0), up);
-                        }
-                    }
-            cluster.sync();
-        }
-        if (rank == 0) {
-            const int per = kBins / nt;  // nt divides kBins
-            u64 sv = 0, sn = 0;
-            for (int b = tid * per; b < (tid + 1) * per; ++b) {
-                sv += by_mass ? (u64)s.lo[b] + ((u64)s.hi[b] << 32) : s.cnt[b];
-                sn += s.cnt[b];
-            }
-            u64 total, all;
-            u64 at = block_scan(sv, s.red, &total), en = block_scan(sn, s.red2, &all);
-            const u64 need = need_of(total);
-            auto tell = [&](int i, u64 v) {
-                for (int r = 0; r < C; ++r) *remote(&s.found[i], r) = v;
-            };
-            if (tid == 0) {
-                tell(4, total);
-                if (total < need) tell(0, kBins);
-            }
-            for (int b = tid * per; b < (tid + 1) * per; ++b) {
-                const u64 v = by_mass ? (u64)s.lo[b] + ((u64)s.hi[b] << 32) : s.cnt[b];
-                en += s.cnt[b];
-                if (at < need && need <= at + v) {
-                    tell(0, b);
-                    tell(1, need - at);
-                    tell(2, s.cnt[b]);
-                    tell(3, en);
-                }
-                at += v;
-            }
-        }
-        all_sync();
+    // Where the search stands: within what `cut` keeps, level 0 looks at all elements by their bins; the
+    // next ones at those of one bin, by `width` bits of the place from `shift` on, the bits above being
+    // `prefix`.
+    constexpr int kPlaceBits = 32 + kIdxBits;
+    int level = 0, shift = kPlaceBits, width = 0, bin = 0;
+    u64 prefix = 0;
+    auto slot_of = [&](float x, int i) {
+        if (level == 0) return cut && place(x, i) < cut ? -1 : bin_of(x);
+        const u64 c = place(x, i);
+        if (c < cut || bin_of(x) != bin || (c >> (shift + width)) != prefix) return -1;
+        // (slots ascend as the order does: the largest place first)
+        return (1 << width) - 1 - (int)((c >> shift) & ((1u << width) - 1));
     };
-    // Elements of bins first .. last with `take` go to CTA 0's list (as many as it holds), the other CTAs'
-    // by way of their own (an atomic a element across the cluster stalls its warp for 1500 cycles).
-    auto gather = [&](int first, int last, auto take) {
-        // (bounds outside the bins' edges spare most elements the exact test)
-        const float slack = fabsf(top) * 0x1p-20f;
-        auto edge = [&](int b, float e) { return top - b / scale * (1.f - e) + e * slack; };
-        const float lo = last >= kBins - 1 || !(scale > 0.f) ? -INFINITY : edge(last + 1, -0x1p-18f) - slack;
-        const float hi = first <= 1 || !(scale > 0.f) ? INFINITY : edge(first, 0x1p-18f) + slack;
-        constexpr int kPer = Row<DT>::kPer;
-        const int chunks = (row.n + kPer - 1) / kPer;
-#pragma unroll 2
-        for (int c = tid; c < chunks; c += nt) {
-            const uint4 u = row.raw(c);
-            typedef Logits<DT> L;
-            if (L::largest(L::larger(L::larger(u.x, u.y), L::larger(u.z, u.w))) < lo) continue;
-            float x[kPer];
-            L::unpack(u, x);
-#pragma unroll
-            for (int k = 0; k < kPer; ++k)
-                if (x[k] >= lo && x[k] <= hi) {
-                    const int b = bin_of(x[k]), i = row.i0 + kPer * c + k;
-                    if (b >= first && b <= last && take(x[k], i)) {
-                        const uint32_t at = atomicAdd(&s.n_list, 1u);
-                        if (at < kList) s.list[at] = place(x[k], i);
-                    }
-                }
-        }
-        if (C > 1) {
-            if (rank != 0) {
-                __syncthreads();
-                const uint32_t n = s.n_list;
-                if (tid == 0 && n) s.first = atomicAdd(remote(&s.n_list, 0), n);
-                __syncthreads();
-                u64* list = remote(s.list, 0);
-                for (uint32_t i = tid; i < min(n, (uint32_t)kList); i += nt)
-                    if (s.first + i < kList) list[s.first + i] = s.list[i];
-                if (tid == 0) s.n_list = 0;
-            }
-            cluster.sync();
-        } else {
-            __syncthreads();
-        }
-    };
-    // Weights and counts of the elements with `take` into the bins.
-    auto count_mass = [&](auto take) {
-        if (weight.fast) {
+    // Counts, and weights where asked for, into the bins.
+    auto count = [&](bool by_mass) {
+        if (by_mass && weight.fast) {
             // in two parts of 20 bits, added without waiting; a bin of 4096 elements could wrap
             row.each([&](float x, int i) {
                 uint32_t h, l;
                 weight.parts(x, h, l);
-                const int b = take(x, i);
+                const int b = slot_of(x, i);
                 if (b < 0) return;
                 atomicAdd(&s.cnt[b], 1u);
                 atomicAdd(&s.lo[b], l - Weights::kBias);
@@ -566,130 +481,218 @@ __global__ void __launch_bounds__(1024) sample_kernel(const SampleParams p) {
             clear_bins();
             __syncthreads();
         }
-        row.each([&](float x, int i) {
-            const int b = take(x, i);
-            if (b < 0) return;
-            add_mass(b, weight(x));
+        const int chunks = (row.n + Row<DT>::kPer - 1) / Row<DT>::kPer * Row<DT>::kPer;
+#pragma unroll 4
+        for (int e = tid; e < chunks; e += nt) {
+            const float x = e < row.n ? Logits<DT>::at(row.src, e) : -INFINITY;
+            const int b = slot_of(x, row.i0 + e);
+            if (b < 0) continue;
+            if (by_mass) add_mass(b, weight(x));
             atomicAdd(&s.cnt[b], 1u);
-        });
+        }
     };
-
-    // The cut of the shortest prefix, within what is kept, that reaches need_of(sum) elements or weight.
-    // True: the whole prefix is in CTA 0's list (n_list elements, some past it), and `total` is the sum
-    // that it is measured by; false: `cut` is set.
-    u64 total = 0;
-    auto find = [&](bool by_mass, auto need_of) {
-        // (weights vanish 27.8 t below the maximum)
-        scale = kBins / (by_mass ? 28.f * t_in : 64.f);
-        const bool all = cut == 0;
-        if (by_mass)
-            count_mass([&](float x, int i) { return all || place(x, i) >= cut ? bin_of(x) : -1; });
-        else
-            row.each([&](float x, int i) { atomicAdd(&s.cnt[bin_of(x)], 1u); });
-        find_bin(by_mass, need_of);
-        total = s.found[4];
-        const int bin = (int)s.found[0];
-        if (s.found[3] <= kList) {
-            gather(0, bin, [&](float x, int i) { return all || place(x, i) >= cut; });
-            return true;
+    // The cluster's bins, added up in CTA 0: prefix sums of counts or weights, and the bin where they
+    // reach `need` (0: top-p's part of the sum over all bins).  found, in all CTAs: bin, what is left of
+    // the need in it, the elements of the bin, the elements up to and with it, the sum.
+    auto find_bin = [&](bool by_mass, u64 need) {
+        all_sync();
+        if (C > 1) {
+            if (rank != 0)
+#pragma unroll 1
+                for (int b = tid; b < kBins; b += nt)
+                    if (s.cnt[b]) {
+                        atomicAdd(remote(&s.cnt[b], 0), s.cnt[b]);
+                        if (by_mass) {
+                            const uint32_t w = s.lo[b], old = atomicAdd(remote(&s.lo[b], 0), w);
+                            const uint32_t up = s.hi[b] + (old + w < old);
+                            if (up) atomicAdd(remote(&s.hi[b], 0), up);
+                        }
+                    }
+            cluster.sync();
         }
-        u64 prefix = 0, need = s.found[1];
-        int shift = 32 + kIdxBits, width = 0;
-        while (s.found[2] > kList) {  // refine by the next bits of the place
-            width = shift > 11 ? 11 : shift;
-            shift -= width;
-            __syncthreads();
-            clear_bins();
-            __syncthreads();
-            auto digit = [&](float x, int i) {
-                const u64 c = place(x, i);
-                if (c < cut || bin_of(x) != bin || (c >> (shift + width)) != prefix) return -1;
-                // (bins ascend as the order does: the largest place first)
-                return (1 << width) - 1 - (int)((c >> shift) & ((1u << width) - 1));
-            };
-            if (by_mass)
-                count_mass(digit);
-            else
-                row.each([&](float x, int i) {
-                    const int b = digit(x, i);
-                    if (b >= 0) atomicAdd(&s.cnt[b], 1u);
-                });
-            find_bin(by_mass, [&](u64) { return need; });
-            prefix = prefix << width | (u64)((1 << width) - 1 - (int)s.found[0]);
-            need = s.found[1];
-        }
-        gather(bin, bin, [&](float x, int i) {
-            const u64 c = place(x, i);
-            return c >= cut && (shift == 32 + kIdxBits || (c >> shift) == prefix);
-        });
         if (rank == 0) {
-            const int n = (int)s.n_list;
-            sort_list(s.list, n, true);
-            const int per = (n + nt - 1) / nt;
-            u64 sum = 0, all_of;
-            for (int i = tid * per; i < min(n, (tid + 1) * per); ++i)
-                sum += by_mass ? weight(place_logit(s.list[i])) : 1;
-            u64 at = block_scan(sum, s.red, &all_of);
-            for (int i = tid * per; i < min(n, (tid + 1) * per); ++i) {
-                const u64 v = by_mass ? weight(place_logit(s.list[i])) : 1;
+            const int per = kBins / nt;  // nt divides kBins
+            u64 sv = 0, sn = 0, sum, all;
+#pragma unroll 1
+            for (int b = tid * per; b < (tid + 1) * per; ++b) {
+                sv += by_mass ? (u64)s.lo[b] + ((u64)s.hi[b] << 32) : s.cnt[b];
+                sn += s.cnt[b];
+            }
+            u64 at = block_scan(sv, s.red, &sum), en = block_scan(sn, s.red2, &all);
+            if (need == 0) need = max((u64)1, part(sum, pf));
+#pragma unroll 1
+            for (int b = tid * per; b < (tid + 1) * per; ++b) {
+                const u64 v = by_mass ? (u64)s.lo[b] + ((u64)s.hi[b] << 32) : s.cnt[b];
+                en += s.cnt[b];
                 if (at < need && need <= at + v)
-                    for (int r = 0; r < C; ++r) *remote(&s.cut, r) = s.list[i];
+#pragma unroll 1
+                    for (int r = 0; r < C; ++r) {
+                        u64* f = remote(s.found, r);
+                        f[0] = b;
+                        f[1] = need - at;
+                        f[2] = s.cnt[b];
+                        f[3] = en;
+                        f[4] = sum;
+                    }
                 at += v;
             }
+        }
+        all_sync();
+    };
+    // Elements of bins first .. last (and of `prefix`, within what is kept) go to CTA 0's list (n_all, or as
+    // many as it holds), the other CTAs' by way of their own (an atomic a element across the cluster stalls
+    // its warp for 1500 cycles).
+    uint32_t n_all = 0;
+    auto gather = [&](int first, int last) {
+        // (bounds outside the bins' edges spare most elements the exact test)
+        const float slack = fabsf(top) * 0x1p-20f;
+        auto edge = [&](int b, float e) { return top - b / scale * (1.f - e) + e * slack; };
+        const float lo = last >= kBins - 1 || !(scale > 0.f) ? -INFINITY : edge(last + 1, -0x1p-18f) - slack;
+        const float hi = first <= 1 || !(scale > 0.f) ? INFINITY : edge(first, 0x1p-18f) + slack;
+        constexpr int kPer = Row<DT>::kPer;
+        const int chunks = (row.n + kPer - 1) / kPer;
+#pragma unroll 2
+        for (int c = tid; c < chunks; c += nt) {
+            const uint4 u = row.raw(c);
+            typedef Logits<DT> L;
+            if (L::largest(L::larger(L::larger(u.x, u.y), L::larger(u.z, u.w))) < lo) continue;
+            float x[kPer];
+            L::unpack(u, x);
+#pragma unroll
+            for (int k = 0; k < kPer; ++k)
+                if (x[k] >= lo && x[k] <= hi) {
+                    const int b = bin_of(x[k]);
+                    const u64 at_place = place(x[k], row.i0 + kPer * c + k);
+                    if (b >= first && b <= last && at_place >= cut &&
+                        (shift == kPlaceBits || (at_place >> shift) == prefix)) {
+                        const uint32_t at = atomicAdd(&s.n_list, 1u);
+                        if (at < kList) s.list[at] = at_place;
+                    }
+                }
+        }
+        __syncthreads();
+        const uint32_t n = s.n_list;
+        n_all = n;
+        if (C > 1) {
+            if (tid < C) remote(s.counts, tid)[rank] = n;
+            cluster.sync();
+            uint32_t before = 0;
+            n_all = 0;
+            for (int r = 0; r < C; ++r) {
+                if (r < rank) before += s.counts[r];
+                n_all += s.counts[r];
+            }
+            u64* list = remote(s.list, 0);
+            if (rank != 0)
+                for (uint32_t i = tid; i < n && before + i < kList; i += nt)
+                    list[before + i] = s.list[i];
+            if (tid == 0) s.n_list = 0;
+            cluster.sync();
+        } else {
+            __syncthreads();
             if (tid == 0) s.n_list = 0;
         }
-        __syncthreads();
-        clear_bins();
-        all_sync();
-        cut = s.cut;
-        return false;
     };
-    // k elements at least, and hardly more: each CTA's bin up to which the maxima of k / C of its threads
-    // lie, and of these bins the last.  False if that does not work out.
-    auto find_small_k = [&] {
-        scale = kBins / 64.f;
-        if (thread_top > -INFINITY) atomicAdd(&s.cnt[bin_of(thread_top)], 1u);
-        if (tid == 0) s.found[0] = kBins;
-        __syncthreads();
-        const u64 need = (u64)(k + C - 1) / C;
-        const int per = kBins / nt;
-        u64 sum = 0, all;
-        for (int b = tid * per; b < (tid + 1) * per; ++b) sum += s.cnt[b];
-        u64 at = block_scan(sum, s.red, &all);
-        for (int b = tid * per; b < (tid + 1) * per; ++b) {
-            if (at < need && need <= at + s.cnt[b]) s.found[0] = b;
-            at += s.cnt[b];
-        }
-        __syncthreads();
-        if (tid < C) remote(s.ends, tid)[rank] = (float)s.found[0];
-        all_sync();
-        float bin = s.ends[0];
-        for (int r = 1; r < C; ++r) bin = fmaxf(bin, s.ends[r]);
-        if (bin < kBins - 1) {
-            gather(0, (int)bin, [](float, int) { return true; });
-            if (*remote(&s.n_list, 0) <= kList) return true;
+
+    // ---- the cuts ----  phase 0: a small top-k, 1: top-k, 2: top-p
+    u64 total = 0;          // the sum that top-p's part is of, where it is not top-k's list's
+    bool in_list = false;   // CTA 0's list has all that can be kept (n_all elements, some not kept)
+    for (int phase = k < V ? k <= kSmallK ? 0 : 1 : use_p ? 2 : 3; phase < 3;) {
+        bool whole = true;
+        level = 0;
+        shift = kPlaceBits;
+        if (phase == 0) {
+            // k elements at least, and hardly more: each CTA's bin up to which the maxima of k / C of its
+            // threads lie, and of these bins the last
+            scale = kBins / 64.f;
+            if (thread_top > -INFINITY) atomicAdd(&s.cnt[bin_of(thread_top)], 1u);
+            if (tid == 0) s.found[0] = kBins;
+            __syncthreads();
+            const u64 need = (u64)((k + C - 1) / C);
+            const int per = kBins / nt;
+            u64 sum = 0, all;
+#pragma unroll 1
+            for (int b = tid * per; b < (tid + 1) * per; ++b) sum += s.cnt[b];
+            u64 at = block_scan(sum, s.red, &all);
+#pragma unroll 1
+            for (int b = tid * per; b < (tid + 1) * per; ++b) {
+                if (at < need && need <= at + s.cnt[b]) s.found[0] = b;
+                at += s.cnt[b];
+            }
+            __syncthreads();
+            if (tid < C) remote(s.ends, tid)[rank] = (float)s.found[0];
             all_sync();
+            float most = s.ends[0];
+            for (int r = 1; r < C; ++r) most = fmaxf(most, s.ends[r]);
+            bin = (int)most;
+        } else {
+            // (weights vanish 27.8 t below the maximum)
+            const bool by_mass = phase == 2;
+            scale = kBins / (by_mass ? 28.f * t_in : 64.f);
+            u64 need = by_mass ? 0 : (u64)k;
+            prefix = 0;
+#pragma unroll 1
+            for (;; ++level) {
+                count(by_mass);
+                find_bin(by_mass, need);
+                const int at = (int)s.found[0];
+                need = s.found[1];
+                if (level == 0) {
+                    total = s.found[4];
+                    bin = at;
+                    whole = s.found[3] <= kList;
+                } else {
+                    prefix = prefix << width | (u64)((1 << width) - 1 - at);
+                }
+                if (whole || s.found[2] <= kList) break;
+                width = shift > 11 ? 11 : shift;  // refine by the next bits of the place
+                shift -= width;
+                __syncthreads();
+                clear_bins();
+                __syncthreads();
+            }
+            if (rank == 0 && tid == 0) s.need = need;
         }
-        if (rank == 0 && tid == 0) s.n_list = 0;
+        if (phase > 0 || bin < kBins - 1) gather(whole ? 0 : bin, bin);
+        if (phase == 0) {
+            in_list = bin < kBins - 1 && n_all <= kList;
+            if (in_list) break;
+            phase = 1;
+        } else if (whole) {
+            in_list = true;
+            break;
+        } else {
+            if (rank == 0) {  // the bin's elements in order: the one that reaches what is left of the need
+                const int n = (int)n_all;
+                const u64 need = s.need;
+                sort_list(s.list, n, true);
+                const int per = kList / nt, j0 = tid * per;
+                u64 sum = 0, all;
+#pragma unroll 1
+                for (int i = j0; i < min(n, j0 + per); ++i) {
+                    s.w[i] = phase == 2 ? weight(place_logit(s.list[i])) : 1;
+                    sum += s.w[i];
+                }
+                u64 at = block_scan(sum, s.red, &all);
+#pragma unroll 1
+                for (int i = j0; i < min(n, j0 + per); ++i) {
+                    if (at < need && need <= at + s.w[i])
+                        for (int r = 0; r < C; ++r) *remote(&s.cut, r) = s.list[i];
+                    at += s.w[i];
+                }
+            }
+            all_sync();
+            cut = s.cut;
+            phase = phase == 1 && use_p ? 2 : 3;
+        }
+        __syncthreads();
         clear_bins();
         all_sync();
-        return false;
-    };
-    bool in_list = false;
-    if (k < V) {
-        in_list = k <= kSmallK && find_small_k();
-        if (!in_list) in_list = find(false, [&](u64) { return (u64)k; });
     }
-    if (use_p && !in_list)
-        in_list = find(true, [&](u64 sum) { return max((u64)1, part(sum, pf)); });
 
     if (in_list) {  // CTA 0 has all that can be kept
-        if (rank != 0) {
-            all_sync();  // (its list length may still be read)
-            return;
-        }
-        int n = (int)s.n_list;
-        all_sync();
+        if (rank != 0) return;
+        int n = (int)n_all;
         const bool by_k = k < V;
         const bool second = cut != 0;  // the list is top-p's, of what top-k kept
         if (n <= kPairs) {
@@ -702,11 +705,12 @@ __global__ void __launch_bounds__(1024) sample_kernel(const SampleParams p) {
                 const u64 mine = i < n ? s.list[i] : 0;
                 u64 before = 0;
                 int rank_i = 0;
-                for (int j = q; j < n; j += 4)
-                    if (s.list[j] > mine) {
-                        before += s.w[j];
-                        ++rank_i;
-                    }
+#pragma unroll 4
+                for (int j = q; j < n; j += 4) {
+                    const u64 c = s.list[j], w = s.w[j];
+                    before += c > mine ? w : 0;
+                    rank_i += c > mine;
+                }
 #pragma unroll
                 for (int o = 1; o < 4; o *= 2) {
                     before += __shfl_xor_sync(0xffffffffu, before, o);
@@ -732,10 +736,11 @@ __global__ void __launch_bounds__(1024) sample_kernel(const SampleParams p) {
                 const int i = i0 + (tid >> 2);
                 const int idx = i < n ? place_index(s.list[i]) : 0;
                 u64 before = 0, all = 0;
+#pragma unroll 4
                 for (int j = q; j < n; j += 4) {
                     const u64 w = s.list[3 * kPairs + j];
                     all += w;
-                    if (place_index(s.list[j]) < idx) before += w;
+                    before += place_index(s.list[j]) < idx ? w : 0;
                 }
 #pragma unroll
                 for (int o = 1; o < 4; o *= 2) {
@@ -754,6 +759,7 @@ __global__ void __launch_bounds__(1024) sample_kernel(const SampleParams p) {
         if (by_k) n = min(n, (int)k);
         const int per = kList / nt, j0 = tid * per;
         u64 sum = 0, all;
+#pragma unroll 1
         for (int i = j0; i < j0 + per; ++i) {
             const u64 w = i < n ? weight(place_logit(s.list[i])) : 0;
             s.w[i] = w;
@@ -762,6 +768,7 @@ __global__ void __launch_bounds__(1024) sample_kernel(const SampleParams p) {
         u64 at = block_scan(sum, s.red, &all);
         const u64 target = !use_p ? ~(u64)0 : max((u64)1, part(by_k && !second ? all : total, pf));
         u64 kept = 0, n_kept;  // a prefix
+#pragma unroll 1
         for (int i = j0; i < j0 + per; ++i) {
             if (i < n && at < target && s.w[i] >= floor_w) ++kept;
             at += s.w[i];
@@ -776,6 +783,7 @@ __global__ void __launch_bounds__(1024) sample_kernel(const SampleParams p) {
         __syncthreads();
         sort_list(s.list, n, false);
         sum = 0;
+#pragma unroll 1
         for (int i = j0; i < j0 + per; ++i) {
             const u64 w = i < n ? weight(logit_of((uint32_t)s.list[i])) : 0;
             s.w[i] = w;
@@ -783,6 +791,7 @@ __global__ void __launch_bounds__(1024) sample_kernel(const SampleParams p) {
         }
         at = block_scan(sum, s.red, &all);
         const u64 draw = part(all, uf);
+#pragma unroll 1
         for (int i = j0; i < j0 + per; ++i) {
             if (at <= draw && draw < at + s.w[i]) {
                 p.out[m] = (int32_t)(s.list[i] >> 32);
