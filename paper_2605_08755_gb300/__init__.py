@@ -2,12 +2,17 @@
 
 The product is ``liblaq.so`` (C ABI in include/laq.h, CUDA for sm_103a).  This package is its
 thin Python binding (``_lib``) plus the decode-step weight pass harness (``weight_pass``) that
-captures the 252 per-token GEMV launches of a Qwen3-shaped decoder into one CUDA graph.
+captures the 252 per-token GEMV launches of a Qwen3-shaped decoder into one CUDA graph, the decode
+step around them (``decode_step``) and a serving step over a paged cache (``paged_step``).
 """
-from ._lib import (EXPORTS, Chain, GemmConfig, LaqError, chain_status, chain_workspace,  # noqa
-                   laq_chain_workspace_bytes, laq_gemm_chain, laq_gemm_plan, laq_gemm_wxg128,
-                   laq_pack, laq_quantize_rtn, laq_unpack, lib, packed_bytes)
+from ._lib import (EXPORTS, Chain, GemmConfig, LaqError, PagedCache, chain_status,  # noqa
+                   chain_workspace, laq_chain_workspace_bytes, laq_gemm_chain, laq_gemm_plan,
+                   laq_gemm_wxg128, laq_pack, laq_paged_append, laq_paged_attention,
+                   laq_quantize_rtn, laq_sample, laq_unpack, lib, packed_bytes,
+                   paged_attention_workspace)
 
-__all__ = ["EXPORTS", "Chain", "GemmConfig", "LaqError", "chain_status", "chain_workspace",
-           "laq_chain_workspace_bytes", "laq_gemm_chain", "laq_gemm_plan", "laq_gemm_wxg128",
-           "laq_pack", "laq_quantize_rtn", "laq_unpack", "lib", "packed_bytes"]
+__all__ = ["EXPORTS", "Chain", "GemmConfig", "LaqError", "PagedCache", "chain_status",
+           "chain_workspace", "laq_chain_workspace_bytes", "laq_gemm_chain", "laq_gemm_plan",
+           "laq_gemm_wxg128", "laq_pack", "laq_paged_append", "laq_paged_attention",
+           "laq_quantize_rtn", "laq_sample", "laq_unpack", "lib", "packed_bytes",
+           "paged_attention_workspace"]

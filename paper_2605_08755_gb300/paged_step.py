@@ -1,0 +1,203 @@
+"""A serving step over a paged cache: requests with any number of new tokens each, sampled choices.
+
+    python -m paper_2605_08755_gb300.paged_step [--layers 4] [--requests 8] [--prompt 700] [--chunk 256]
+
+``PagedStep`` runs the decoder of ``DecodeStep`` (its synthetic Qwen3-shaped weights, quantized
+projections and norms) for a batch in which every request brings a prompt, a chunk of one, or the
+token it has just sampled:
+
+    x = embed(tokens)                                          [T rows of all requests]
+    per layer:  h = rmsnorm(r);  qkv = h Wqkv
+                q = laq_paged_append(qkv)                       (norms, rotation, k and v to the pages)
+                a = laq_paged_attention(q)                      (causal, over each request's pages)
+                h = rmsnorm(r += a Wo);  r += silu(gate) * up Wdown
+    logits of each request's last row;  laq_sample(logits, u)
+
+The projections take rows in slabs of 16, the most of one laq_gemm_wxg128 call.  The caller owns the
+pages: it says which ones a request holds and how long it is (``PagedPool`` below hands them out).  The
+program at the end prefills requests chunk by chunk beside ones that already decode, as a server does.
+"""
+import argparse
+import time
+
+import torch
+
+from . import _lib
+from .decode_step import DecodeStep
+
+SLAB = 16  # most rows of a projection call
+
+
+class PagedPool:
+    """Which pages belong to which request: host bookkeeping, and the tables that the kernels read."""
+
+    def __init__(self, requests, pages, page_size, max_pages, device):
+        self.page_size = page_size
+        self.free = list(range(pages - 1, -1, -1))
+        self.held = [[] for _ in range(requests)]
+        self.length = [0] * requests
+        self.table = torch.full((requests, max_pages), -1, dtype=torch.int32, device=device)
+        self.q_start = torch.zeros((requests + 1,), dtype=torch.int32, device=device)
+        self.kv_len = torch.zeros((requests,), dtype=torch.int32, device=device)
+
+    def extend(self, counts):
+        """Request b gets counts[b] more tokens: pages for them, and the tables of the coming step."""
+        wants = [-(-(have + n) // self.page_size) for have, n in zip(self.length, counts)]
+        if max(wants, default=0) > self.table.shape[1]:
+            raise ValueError("a request's tokens exceed its table")
+        if sum(w - len(h) for w, h in zip(wants, self.held)) > len(self.free):
+            raise ValueError("out of pages")
+        for b, (n, want) in enumerate(zip(counts, wants)):
+            self.length[b] += n
+            first = len(self.held[b])
+            if want > first:
+                new = [self.free.pop() for _ in range(want - first)]
+                self.held[b] += new
+                self.table[b, first:want] = torch.tensor(new, dtype=torch.int32)
+        starts = [0]
+        for n in counts:
+            starts.append(starts[-1] + n)
+        self.q_start.copy_(torch.tensor(starts, dtype=torch.int32))
+        self.kv_len.copy_(torch.tensor(self.length, dtype=torch.int32))
+
+    def release(self, b):
+        """Request b has ended: its pages are free, its row empty."""
+        self.free += self.held[b]
+        self.held[b], self.length[b] = [], 0
+        self.table[b].fill_(-1)
+
+
+class PagedStep:
+    """``weights``: a DecodeStep whose projections, norms, embedding and LM head are used;
+    ``max_rows`` / ``max_q``: the most rows of a step, and of one request in it."""
+
+    def __init__(self, weights: DecodeStep, requests, max_rows, max_q, pages, page_size=64,
+                 max_pages=None):
+        w = self.w = weights
+        dev = w.device
+        self.pool = PagedPool(requests, pages, page_size, max_pages or pages, dev)
+        shape = (pages, w.Hkv, page_size, w.D)
+        f16 = dict(dtype=torch.float16, device=dev)
+        self.caches = []
+        for _ in range(w.layers):
+            k, v = torch.empty(shape, **f16), torch.empty(shape, **f16)
+            self.caches.append(_lib.PagedCache(k, v, self.pool.table, self.pool.q_start,
+                                               self.pool.kv_len))
+        self.ws = _lib.paged_attention_workspace(max_rows, requests, max_q, w.Hq, w.Hkv, dev)
+        T = self.max_rows = max_rows
+        self.requests, self.max_q = requests, max_q
+        self.x = torch.empty((T, w.H), **f16)
+        self.r = torch.empty((T, w.H), **f16)
+        self.h = torch.empty((T, w.H), **f16)
+        self.qkv = torch.empty((T, (w.Hq + 2 * w.Hkv) * w.D), **f16)
+        self.q = torch.empty((T, w.Hq, w.D), **f16)
+        self.att = torch.empty((T, w.Hq, w.D), **f16)
+        self.d = torch.empty((T, w.H), **f16)
+        self.gu = torch.empty((T, 2 * w.I), **f16)
+        self.act = torch.empty((T, w.I), **f16)
+        self.last = torch.empty((requests, w.H), **f16)
+        self.logits = torch.empty((requests, w.V), **f16)
+        self.next = torch.zeros((requests,), dtype=torch.int32, device=dev)
+        self.prob = torch.empty((requests,), dtype=torch.float32, device=dev)
+
+    def project(self, X, lin, Y, stream=None):
+        for i in range(0, X.shape[0], SLAB):
+            _lib.laq_gemm_wxg128(X[i:i + SLAB], lin.packed, lin.s, lin.z, lin.bits, Y=Y[i:i + SLAB],
+                                 stream=stream)
+
+    def run(self, tokens, counts, u, temperature=None, top_k=None, top_p=None, min_p=None, stream=None):
+        """One step: ``tokens`` int32 [T] on the device, request b's counts[b] next ones after
+        another (0: the request waits).  Extends the requests and returns ``next`` int32 [requests],
+        the token sampled after each request's last row (meaningless where counts[b] is 0)."""
+        L, w, T = _lib, self.w, tokens.shape[0]
+        if len(counts) != self.requests or sum(counts) != T or T > self.max_rows:
+            raise ValueError("counts [requests] that add up to the tokens, at most max_rows, expected")
+        if max(counts, default=0) > self.max_q:
+            raise ValueError("more new tokens of a request than max_q")
+        self.pool.extend(counts)
+        if T == 0:
+            return self.next
+        x, r, h, d = self.x[:T], self.r[:T], self.h[:T], self.d[:T]
+        qkv, q, att, gu, act = self.qkv[:T], self.q[:T], self.att[:T], self.gu[:T], self.act[:T]
+        most = max(counts)
+        L.laq_embed(w.E, tokens, X=x, stream=stream)
+        for l in range(w.layers):
+            nw, (pqkv, po, pgu, pdn) = w.norms[l], w.proj[l]
+            if l == 0:
+                L.laq_rmsnorm(x, nw["in_w"], w.eps, R_out=r, Y=h, stream=stream)
+            else:
+                L.laq_rmsnorm(d, nw["in_w"], w.eps, R=r, R_out=r, Y=h, stream=stream)
+            self.project(h, pqkv, qkv, stream)
+            L.laq_paged_append(qkv, self.caches[l], w.Hq, w.theta, w.eps, q_norm_w=nw["q_w"],
+                               k_norm_w=nw["k_w"], q_out=q, stream=stream)
+            L.laq_paged_attention(q, self.caches[l], most, w.scale, self.ws, out=att, stream=stream)
+            self.project(att.view(T, -1), po, d, stream)
+            L.laq_rmsnorm(d, nw["post_w"], w.eps, R=r, R_out=r, Y=h, stream=stream)
+            self.project(h, pgu, gu, stream)
+            L.laq_silu_mul(gu, h=act, stream=stream)
+            self.project(act, pdn, d, stream)
+        # (a request's last row; one that waits: row -1 of no request, which the gather reads as zeros)
+        ends = [sum(counts[:b + 1]) - 1 if n else -1 for b, n in enumerate(counts)]
+        rows = torch.tensor(ends, dtype=torch.int32, device=w.device)
+        L.laq_rmsnorm(d, w.final_w, w.eps, R=r, Y=h, stream=stream)
+        L.laq_embed(h, rows, X=self.last, stream=stream)
+        self.project(self.last, w.lm, self.logits, stream)
+        return L.laq_sample(self.logits, u, temperature=temperature, top_k=top_k, top_p=top_p,
+                            min_p=min_p, out=self.next, p_out=self.prob, stream=stream)
+
+
+def main():
+    ap = argparse.ArgumentParser()
+    ap.add_argument("--model", default="qwen3-4b")
+    ap.add_argument("--layers", type=int, default=4)
+    ap.add_argument("--vocab", type=int, default=None)
+    ap.add_argument("--requests", type=int, default=8)
+    ap.add_argument("--prompt", type=int, default=700)
+    ap.add_argument("--chunk", type=int, default=256)
+    ap.add_argument("--new", type=int, default=16, help="tokens to sample per request")
+    a = ap.parse_args()
+    ds = DecodeStep(model=a.model, layers=a.layers, context=1, vocab=a.vocab)
+    dev, B = ds.device, a.requests
+    total = a.prompt + a.new
+    pages = B * -(-total // 64) + 1
+    st = PagedStep(ds, B, a.chunk + B, a.chunk, pages, max_pages=-(-total // 64))
+    g = torch.Generator(device=dev).manual_seed(1)
+    prompts = torch.randint(0, ds.V, (B, a.prompt), generator=g, device=dev, dtype=torch.int32)
+    settings = dict(temperature=torch.full((B,), 0.8, device=dev),
+                    top_k=torch.full((B,), 50, dtype=torch.int32, device=dev),
+                    top_p=torch.full((B,), 0.95, device=dev))
+    fed, got, out = [0] * B, [0] * B, [[] for _ in range(B)]
+    torch.cuda.synchronize()
+    t0, steps, rows = time.perf_counter(), 0, 0
+    while min(got) < a.new:
+        # requests that have their prompt decode; the first that has not gets its next chunk
+        counts, parts, waiting = [0] * B, [], True
+        for b in range(B):
+            if fed[b] < a.prompt:
+                if waiting:
+                    counts[b] = min(a.chunk, a.prompt - fed[b])
+                    parts.append(prompts[b, fed[b]:fed[b] + counts[b]])
+                    waiting = False
+            elif got[b] < a.new:
+                counts[b] = 1
+                parts.append(st.next[b:b + 1].clone())
+        u = torch.rand((B,), generator=g, device=dev)
+        nxt = st.run(torch.cat(parts), counts, u, **settings).tolist()
+        for b, n in enumerate(counts):
+            if fed[b] < a.prompt:
+                fed[b] += n
+                done = n > 0 and fed[b] == a.prompt
+            else:
+                done = n > 0
+            if done:
+                out[b].append(nxt[b])
+                got[b] += 1
+        steps, rows = steps + 1, rows + sum(counts)
+    dt = time.perf_counter() - t0
+    print(f"{B} requests, {a.prompt} prompt and {a.new} sampled tokens each: {steps} steps, "
+          f"{rows} rows, {dt:.2f} s ({rows / dt:.0f} rows/s)")
+    print("request 0:", out[0])
+
+
+if __name__ == "__main__":
+    main()
