@@ -9,9 +9,9 @@
 // for the item's two q tiles i = 0, 1, one warpgroup each, so that one tile's exponentials run while
 // the tensor cores work on the other's products.  An item of one q tile gives the two warpgroups the
 // even and the odd tiles of tokens instead and adds the two results at its end.
-//   m_i is the running maximum, moved only when a row's has grown by more than 2^8 since (the sums
-// and O are in units of 2^(c m_i); a P of up to 2^8 more costs nothing in a floating-point type):
-// then the warp rescales its rows of O.  The offset of 2^7 keeps small fp16 P above the subnormals.
+//   m_i is the running maximum, moved only when the exponentials of a row's tile come to more than 2^8
+// (the sums and O are in units of 2^(c m_i); larger P cost nothing in a floating-point type): then the
+// warp rescales its rows of O.  The offset of 2^7 keeps small fp16 P above the subnormals.
 //   K, V and Q come by TMA in the 128-byte swizzle that the products read; pages that end inside a
 // tile are filled by boxes of a page each.  Rows of V past the request's last token are zeroed in
 // shared memory, since 0 * NaN would not vanish in the product.
@@ -48,7 +48,6 @@ constexpr int kSmemTiles = kStaging + 8 * 4096;
 constexpr int kMostCtas = 192;          // so that a row of every part fits beside the others
 constexpr int kMinUnits = 4;            // fewer are not worth a CTA of their own
 constexpr int kStart = 2;               // what starting and ending an item costs, in tiles
-constexpr float kGrow = 8.f;            // how far a maximum may grow before O is rescaled (log2)
 
 // The part of an item that one CTA works on: tiles lo .. hi - 1 of its nt (0: no row of it sees a token;
 // -1: the end of the CTA's share).
@@ -75,11 +74,7 @@ struct Bars {
     uint64_t s_full[2], p_full[2], o_full[2], soft, fetch, work_full[kQueue], work_empty[kQueue];
     Piece queue[kQueue], pend[2];       // pieces in work; split ones that wait for their other parts
     uint32_t tmem, abort;
-    int b;                              // this CTA's share: from unit `into` of request b, which starts at
-    long long into, at, left;           // unit `at`; `left` units
-    Shares shares;
     float2 ml[kTile];                   // (maximum, sum) of the second warpgroup's rows
-    long long scan[kThreads / 32];
 };
 constexpr int kSmem = kSmemTiles + 1024 + (int)sizeof(Bars);
 
@@ -237,66 +232,57 @@ struct Req {
     }
 };
 
-// Every thread takes a run of requests; one of them finds the request where the CTA's share starts.
-__device__ void plan(const ChunkParams& p, Bars* s) {
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int per = (p.kv.batch + kThreads - 1) / kThreads;
-    const int b0 = min(p.kv.batch, tid * per), b1 = min(p.kv.batch, b0 + per);
-    Req r;
-    long long sum = 0;
-#pragma unroll 1
-    for (int b = b0; b < b1; ++b) {
-        r.load(p, b);
-        sum += r.units(p) * p.kv.Hkv;
-    }
-    long long inc = sum;
-#pragma unroll
-    for (int o = 1; o < 32; o *= 2) {
-        const long long y = __shfl_up_sync(0xffffffffu, inc, o);
-        if (lane >= o) inc += y;
-    }
-    if (lane == 31) s->scan[warp] = inc;
-    if (tid == 0) s->left = 0;
-    __syncthreads();
-    long long before = 0, W = 0;
-#pragma unroll 1
-    for (int k = 0; k < kThreads / 32; ++k) {
-        if (k < warp) before += s->scan[k];
-        W += s->scan[k];
-    }
-    before += inc - sum;
-    const int ctas = (int)max(1LL, min((long long)gridDim.x, W / kMinUnits));
-    if (W == 0 || (int)blockIdx.x >= ctas) return;
-    Shares sh;
-    sh.set(W, ctas);
-    const long long u0 = sh.start(blockIdx.x);
-    if (u0 < before || u0 >= before + sum) return;
-    int b = b0;
-#pragma unroll 1
-    for (; b1 - b > 1; ++b) {  // (with one request a thread, it is that)
-        r.load(p, b);
-        const long long c = r.units(p) * p.kv.Hkv;
-        if (u0 < before + c) break;
-        before += c;
-    }
-    s->b = b;
-    s->into = u0 - before;
-    s->at = before;
-    s->left = sh.start(blockIdx.x + 1) - u0;
-    s->shares = sh;
-}
-
 // ---- roles ----
-// Walks the CTA's share and puts its pieces into the queue (a warp: its lanes look for the first item
-// together).
+// Finds the CTA's share, walks it and puts its pieces into the queue (a warp: its lanes look at 32
+// requests, then at 32 items at a time).
 __device__ void walk_role(const ChunkParams& p, Bars* s) {
     const int lane = threadIdx.x & 31;
-    long long left = s->left, U = 0;
-    int b = s->b, g = 0, t = 0, off = 0;
+    long long left = 0, U = 0, into = 0;
+    int b = 0, g = 0, t = 0, off = 0;
     Req r;
+    Shares shares;
+#pragma unroll 1
+    for (int pass = 0, b0 = 0; b0 < p.kv.batch;) {  // all units; then where the share starts
+        long long v = 0, inc;
+        if (b0 + lane < p.kv.batch) {
+            r.load(p, b0 + lane);
+            v = r.units(p) * p.kv.Hkv;
+        }
+        inc = v;
+#pragma unroll 1
+        for (int o = 1; o < 32; o *= 2) {
+            const long long y = __shfl_up_sync(0xffffffffu, inc, o);
+            if (lane >= o) inc += y;
+        }
+        const long long all = __shfl_sync(0xffffffffu, inc, 31);
+        if (pass == 0) {
+            U += all;
+            if ((b0 += 32) < p.kv.batch) continue;
+            const int ctas = (int)max(1LL, min((long long)gridDim.x, div_ll(U, kMinUnits)));
+            if (U == 0 || (int)blockIdx.x >= ctas) break;
+            shares.set(U, ctas);
+            into = shares.start(blockIdx.x);
+            left = shares.start(blockIdx.x + 1) - into;
+            pass = 1;
+            b0 = U = 0;
+            if (p.kv.batch > 32) continue;
+        }
+        if (into >= all) {
+            into -= all;
+            U += all;
+            b0 += 32;
+            continue;
+        }
+        const int c = __popc(__ballot_sync(0xffffffffu, inc <= into));
+        const long long before = __shfl_sync(0xffffffffu, inc - v, c);
+        b = b0 + c;
+        into -= before;
+        U += before;
+        break;
+    }
     if (left > 0) {
         r.load(p, b);
-        long long into = s->into, per_head = 0;
+        long long per_head = 0;
         // the warp adds up the items' units, 32 items at a time; a second time to find `into`
 #pragma unroll 1
         for (int pass = 0, t0 = 0;;) {
@@ -312,7 +298,7 @@ __device__ void walk_role(const ChunkParams& p, Bars* s) {
                 if ((t0 += 32) < r.m) continue;
                 g = (int)div_ll(into, per_head);
                 into -= g * per_head;
-                U = s->at + g * per_head;
+                U += g * per_head;
                 pass = 1;
                 t0 = 0;
                 if (r.m > 32) continue;
@@ -360,8 +346,8 @@ __device__ void walk_role(const ChunkParams& p, Bars* s) {
                 x->parts = 1;
                 x->index = 0;
                 if (x->split) {
-                    x->first = s->shares.cta_of(U + kStart);
-                    x->parts = s->shares.cta_of(U + kStart + nt - 1) - x->first + 1;
+                    x->first = shares.cta_of(U + kStart);
+                    x->parts = shares.cta_of(U + kStart + nt - 1) - x->first + 1;
                     x->index = (int)blockIdx.x - x->first;
                     s->pend[x->slot] = *x;
                 }
@@ -819,7 +805,7 @@ __device__ void softmax_role(const ChunkParams& p, Bars* s, uint32_t smem, uint8
     const int wg = threadIdx.x >> 7, r = threadIdx.x & 127;
     const uint32_t lanes = (uint32_t)((threadIdx.x >> 5) & 3) << 21;  // the warp's lanes of tensor memory
     const uint32_t ts = tmem + lanes + 128 * wg, to = tmem + lanes + 256 + 128 * wg;
-    const float c = p.scale_log2, offset = BF ? 0.f : 7.f;
+    const float c = p.scale_log2, offset = BF ? 0.f : 7.f, most = BF ? 0x1p8f : 0x1p15f;
     uint32_t ns = 0, no = 0, met = 0, fetched = 0;
     bool ok = true;
     for (uint32_t w = 0; ok; ++w) {
@@ -845,8 +831,9 @@ __device__ void softmax_role(const ChunkParams& p, Bars* s, uint32_t smem, uint8
                 if ((threadIdx.x & 31) == 0) bar_arrive(&s->p_full[wg]);
                 continue;
             }
-            // The exponentials of a tile take the maximum so far on trust, its own being found beside
-            // them; where it has grown too much (and in the first tile) they are taken again.
+            // The exponentials of a tile take the maximum so far on trust.  Had a score grown past it, their
+            // sum would show it (128 scores at the maximum come to 2^7): where it is above 2^8, and in the
+            // first tile, the maximum is found and they are taken again.
             float sum[4];
             uint32_t pk[64];
             for (bool trust = !first;; trust = false) {
@@ -862,8 +849,8 @@ __device__ void softmax_role(const ChunkParams& p, Bars* s, uint32_t smem, uint8
                     for (int e = 0; e < 128; ++e)
                         if (e >= lim) v[e] = -INFINITY;
                 }
-                float mx[4] = {v[0], v[1], v[2], v[3]};
                 if (!trust) {
+                    float mx[4] = {v[0], v[1], v[2], v[3]};
 #pragma unroll
                     for (int e = 4; e < 128; e += 2)
                         mx[(e >> 1) & 3] = max3(mx[(e >> 1) & 3], v[e], v[e + 1]);
@@ -889,7 +876,6 @@ __device__ void softmax_role(const ChunkParams& p, Bars* s, uint32_t smem, uint8
                 sum[0] = sum[1] = sum[2] = sum[3] = 0.f;
 #pragma unroll
                 for (int e = 0; e < 128; e += 2) {
-                    mx[(e >> 1) & 3] = max3(mx[(e >> 1) & 3], v[e], v[e + 1]);
                     fma2(v[e], v[e + 1], c, -base);
                     v[e] = ex2(v[e]);
                     v[e + 1] = ex2(v[e + 1]);
@@ -897,8 +883,7 @@ __device__ void softmax_role(const ChunkParams& p, Bars* s, uint32_t smem, uint8
                     pk[e >> 1] = Half16<BF>::pack(v[e], v[e + 1]);
                 }
                 if (!trust) break;
-                const float mn = fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]);
-                if (!__any_sync(0xffffffffu, valid && (mn - m) * c > kGrow)) break;
+                if (!__any_sync(0xffffffffu, valid && (sum[0] + sum[1]) + (sum[2] + sum[3]) > most)) break;
             }
             first = false;
             tm_st32(ts, pk);
@@ -955,6 +940,11 @@ __global__ void __launch_bounds__(kThreads, 1) paged_chunk_kernel(
     const uint32_t smem = (s32(raw) + 1023u) & ~1023u;
     Bars* s = reinterpret_cast<Bars*>(raw + (smem - s32(raw)) + kSmemTiles);
     const int warp = threadIdx.x >> 5;
+    if (threadIdx.x < 3)
+        asm volatile("prefetch.tensormap [%0];" ::"l"(threadIdx.x == 0   ? &p.qmap
+                                                      : threadIdx.x == 1 ? &p.kmap
+                                                                         : &p.vmap)
+                     : "memory");
     if (threadIdx.x == 0) {
         for (int i = 0; i < kStages; ++i) {
             bar_init(&s->full[i], 1);
@@ -985,7 +975,6 @@ __global__ void __launch_bounds__(kThreads, 1) paged_chunk_kernel(
                      : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
-    plan(p, s);
     tc_before();
     __syncthreads();
     tc_after();

@@ -55,9 +55,7 @@ struct DecodeSmem {
     float2 ml[kDecodeRows];
     uint64_t full[kWarps][kSlots];
     uint32_t abort;
-    int b, g, last;
-    long long at, u0, u1, scan[kWarps];
-    Shares shares;
+    int last;
 };
 constexpr int kRing = kWarps * kSlots * kSlotBytes;
 constexpr int kSmem = kRing + 1024 + (int)sizeof(DecodeSmem);
@@ -104,55 +102,57 @@ struct Request {
     __device__ int units() const { return n == 0 ? 0 : max(1, (len + kUnit - 1) / kUnit); }
 };
 
-// Where this CTA's share starts: its units u0 .. u1 - 1 of W, and the pair that u0 is in (its first
-// unit: at).
-__device__ void plan(const DecodeParams& p, DecodeSmem* s) {
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int per = (p.kv.batch + kThreads - 1) / kThreads;
-    const int b0 = min(p.kv.batch, tid * per), b1 = min(p.kv.batch, b0 + per);
-    Request r;
-    long long sum = 0;
-    for (int b = b0; b < b1; ++b) {
-        r.load(p, b);
-        sum += (long long)r.units() * p.kv.Hkv;
+// This CTA's share, found by every warp on its own (32 requests at a time): its units u0 .. u1 - 1, and the
+// pair that u0 is in, whose first unit is `at`.
+struct Share {
+    Shares all;
+    long long at, u0, u1;
+    int b, g;
+    __device__ __forceinline__ Share(const DecodeParams& p) : at(0), u0(0), u1(0), b(0), g(0) {
+        const int lane = threadIdx.x & 31;
+        Request r;
+#pragma unroll 1
+        for (int pass = 0, b0 = 0; b0 < p.kv.batch;) {
+            int units = 0;
+            if (b0 + lane < p.kv.batch) {
+                r.load(p, b0 + lane);
+                units = r.units();
+            }
+            const long long v = (long long)units * p.kv.Hkv;
+            long long inc = v;
+#pragma unroll 1
+            for (int o = 1; o < 32; o *= 2) {
+                const long long y = __shfl_up_sync(0xffffffffu, inc, o);
+                if (lane >= o) inc += y;
+            }
+            const long long sum = __shfl_sync(0xffffffffu, inc, 31);
+            if (pass == 0) {
+                at += sum;
+                if ((b0 += 32) < p.kv.batch) continue;
+                const int ctas = (int)min((long long)gridDim.x, at);
+                if ((int)blockIdx.x >= ctas) return;
+                all.set(at, ctas);
+                u0 = all.start(blockIdx.x);
+                u1 = all.start(blockIdx.x + 1);
+                pass = 1;
+                b0 = at = 0;
+                if (p.kv.batch > 32) continue;
+            }
+            if (u0 - at >= sum) {
+                at += sum;
+                b0 += 32;
+                continue;
+            }
+            const int c = __popc(__ballot_sync(0xffffffffu, inc <= u0 - at));
+            at += __shfl_sync(0xffffffffu, inc - v, c);
+            units = __shfl_sync(0xffffffffu, units, c);
+            b = b0 + c;
+            g = (int)div_ll(u0 - at, units);
+            at += (long long)g * units;
+            return;
+        }
     }
-    long long inc = sum;
-#pragma unroll
-    for (int o = 1; o < 32; o *= 2) {
-        const long long y = __shfl_up_sync(0xffffffffu, inc, o);
-        if (lane >= o) inc += y;
-    }
-    if (lane == 31) s->scan[warp] = inc;
-    if (tid == 0) s->u0 = s->u1 = 0;
-    __syncthreads();
-    long long before = 0, W = 0;
-    for (int k = 0; k < kWarps; ++k) {
-        if (k < warp) before += s->scan[k];
-        W += s->scan[k];
-    }
-    before += inc - sum;
-    const int ctas = (int)min((long long)gridDim.x, W);
-    if ((int)blockIdx.x >= ctas) return;
-    Shares sh;
-    sh.set(W, ctas);
-    const long long u0 = sh.start(blockIdx.x);
-    if (u0 < before || u0 >= before + sum) return;
-    int b = b0;
-    long long at = before;
-    int units = 0;
-    for (; b < b1; ++b) {
-        r.load(p, b);
-        units = r.units();
-        if (u0 < at + (long long)units * p.kv.Hkv) break;
-        at += (long long)units * p.kv.Hkv;
-    }
-    s->b = b;
-    s->g = (int)div_ll(u0 - at, units);
-    s->at = at + (long long)s->g * units;
-    s->u0 = u0;
-    s->u1 = sh.start(blockIdx.x + 1);
-    s->shares = sh;
-}
+};
 
 template <bool BF, int NT>
 __global__ void __launch_bounds__(kThreads, 2) paged_decode_kernel(
@@ -164,21 +164,23 @@ __global__ void __launch_bounds__(kThreads, 2) paged_decode_kernel(
     DecodeSmem* s = reinterpret_cast<DecodeSmem*>(ring_ptr + kRing);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, c = lane & 3, r8 = lane >> 2;
     pdl_launch_dependents();
+    if (tid < 2)
+        asm volatile("prefetch.tensormap [%0];" ::"l"(tid ? &p.vmap : &p.kmap) : "memory");
     if (tid == 0) {
         for (int w = 0; w < kWarps; ++w)
             for (int i = 0; i < kSlots; ++i) bar_init(&s->full[w][i], 1);
         s->abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    pdl_wait();
-    plan(p, s);
     __syncthreads();
+    pdl_wait();
+    const Share share(p);
     const int P = 1 << p.kv.page_bits, box = min(P, kStep);
     const uint32_t slots = ring + warp * kSlots * kSlotBytes;
     uint32_t seq = 0, issued = 0;  // K, V, K, V .. of the warp's steps: used and asked for so far
-    int b = s->b, g = s->g;
-    long long at = s->at, u = s->u0;
-    const long long u1 = s->u1;
+    int b = share.b, g = share.g;
+    long long at = share.at, u = share.u0;
+    const long long u1 = share.u1;
     Request req;
     if (u < u1) req.load(p, b);
     while (u < u1) {
@@ -411,7 +413,7 @@ __global__ void __launch_bounds__(kThreads, 2) paged_decode_kernel(
         }
         if (!whole) {
             if (tid < rows) __stcg(&p.ml[slot * p.part_rows + tid], s->ml[tid]);
-            const int first = s->shares.cta_of(at), last = s->shares.cta_of(at + units - 1);
+            const int first = share.all.cta_of(at), last = share.all.cta_of(at + units - 1);
             __threadfence();
             __syncthreads();
             if (tid == 0) {
