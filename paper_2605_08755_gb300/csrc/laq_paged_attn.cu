@@ -46,7 +46,7 @@ constexpr int kQueue = 4;
 constexpr int kStaging = (2 + kStages) * kTileBytes;  // where: 4 KB for each softmax warp
 constexpr int kSmemTiles = kStaging + 8 * 4096;
 constexpr int kMostCtas = 192;          // so that a row of every part fits beside the others
-constexpr int kMinUnits = 4;            // fewer are not worth a CTA of their own
+constexpr int kMinUnits = 2;            // for a CTA of its own (or one an item, if that is more CTAs)
 constexpr int kStart = 2;               // what starting and ending an item costs, in tiles
 
 // The part of an item that one CTA works on: tiles lo .. hi - 1 of its nt (0: no row of it sees a token;
@@ -238,7 +238,7 @@ struct Req {
 __device__ void walk_role(const ChunkParams& p, Bars* s) {
     const int lane = threadIdx.x & 31;
     long long left = 0, U = 0, into = 0;
-    int b = 0, g = 0, t = 0, off = 0;
+    int b = 0, g = 0, t = 0, off = 0, items = 0;
     Req r;
     Shares shares;
 #pragma unroll 1
@@ -257,8 +257,10 @@ __device__ void walk_role(const ChunkParams& p, Bars* s) {
         const long long all = __shfl_sync(0xffffffffu, inc, 31);
         if (pass == 0) {
             U += all;
+            items += __reduce_add_sync(0xffffffffu, b0 + lane < p.kv.batch ? r.m * p.kv.Hkv : 0);
             if ((b0 += 32) < p.kv.batch) continue;
-            const int ctas = (int)max(1LL, min((long long)gridDim.x, div_ll(U, kMinUnits)));
+            const long long want = max((long long)items, div_ll(U, kMinUnits));
+            const int ctas = (int)min((long long)gridDim.x, want);
             if (U == 0 || (int)blockIdx.x >= ctas) break;
             shares.set(U, ctas);
             into = shares.start(blockIdx.x);
@@ -613,8 +615,8 @@ __device__ __noinline__ bool add_parts(Bars* s, uint32_t smem, uint8_t* tiles, u
                                        uint32_t& fetched, const Piece& d, int r0, int r1) {
     const Common p = s->c;
     const int narrow = d.narrow, sources = narrow ? 2 * d.parts : d.parts;
-    float* weight = reinterpret_cast<float*>(tiles + kStaging);  // [source][row]: 32 KB
-    const int most = min(kStaging / 512, 8192) / sources;        // rows at a time (sources <= 2 kMostCtas)
+    float2* weight = reinterpret_cast<float2*>(tiles + kStaging);  // [source][row]: its weight
+    const int most = kStaging / 512 / sources;  // rows at a time (sources <= 2 kMostCtas)
     auto place = [&](int k, int r) {                             // of row r in source k
         const int part = narrow ? k >> 1 : k;
         const int half = narrow ? k & 1 : r >= p.per;
@@ -639,45 +641,55 @@ __device__ __noinline__ bool add_parts(Bars* s, uint32_t smem, uint8_t* tiles, u
                     "r"(s32(&s->fetch))
                     : "memory");
         }
-        if (tid < rows) {
+#pragma unroll 1
+        for (int e = tid; e < rows * sources; e += 256) {
+            const int k = e / rows;
+            weight[e] = __ldcg(&p.ml[place(k, r0 + e - k * rows)]);  // (maximum, sum)
+        }
+        const uint32_t turn = fetched++ & 1;
+        bool ok = meet(s, met);
+        if (ok && tid < rows) {
+            float2* ml = weight + tid;
             float M = -INFINITY, l = 0.f;
 #pragma unroll 4
-            for (int k = 0; k < sources; ++k) M = fmaxf(M, __ldcg(&p.ml[place(k, r0 + tid)]).x);
-#pragma unroll 1
+            for (int k = 0; k < sources; ++k) M = fmaxf(M, ml[k * rows].x);
+#pragma unroll 4
             for (int k = 0; k < sources; ++k) {
-                const float2 v = __ldcg(&p.ml[place(k, r0 + tid)]);
+                const float2 v = ml[k * rows];
                 // (no weight: nothing was written)
                 const float f =
                     v.x == -INFINITY && v.y == 0.f ? 0.f : ex2((v.x - M) * p.scale_log2);
-                weight[k * rows + tid] = f;
+                ml[k * rows].x = f;
                 l = fmaf(f, v.y, l);
             }
             const float inv = l == 0.f ? 0.f : 1.f / l;
-#pragma unroll 1
-            for (int k = 0; k < sources; ++k) weight[k * rows + tid] *= inv;
+#pragma unroll 4
+            for (int k = 0; k < sources; ++k) ml[k * rows].x *= inv;
         }
-        const uint32_t turn = fetched++ & 1;
-        if (!meet(s, met) || !warp_wait(s, &s->fetch, turn)) {
+        ok = ok && meet(s, met);
+        if (!ok || !warp_wait(s, &s->fetch, turn)) {
             drain(&s->fetch, turn);
             return false;
         }
+        const int c = tid & 31;
 #pragma unroll 1
-        for (int e = tid; e < rows * 32; e += 256) {
-            const int row = e >> 5, r = r0 + row;
+        for (int row = tid >> 5; row < rows; row += 8) {
+            const float4* src = reinterpret_cast<const float4*>(tiles) + row * 32 + c;
             float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 2
+#pragma unroll 4
             for (int k = 0; k < sources; ++k) {
-                const float f = weight[k * rows + row];
-                const float4 o = reinterpret_cast<const float4*>(tiles)[(k * rows + row) * 32 + (e & 31)];
-                if (f == 0.f) continue;
+                const float f = weight[k * rows + row].x;
+                float4 o = src[k * rows * 32];
+                if (f == 0.f) o = make_float4(0.f, 0.f, 0.f, 0.f);
                 a.x = fmaf(o.x, f, a.x);
                 a.y = fmaf(o.y, f, a.y);
                 a.z = fmaf(o.z, f, a.z);
                 a.w = fmaf(o.w, f, a.w);
             }
+            const int r = r0 + row, token = r / p.G;
             *reinterpret_cast<uint2*>(
-                p.out + ((int64_t)(d.row0 + r / p.G) * p.Hq + d.g * p.G + r % p.G) * kPagedDim +
-                4 * (e & 31)) = make_uint2(Half16<BF>::pack(a.x, a.y), Half16<BF>::pack(a.z, a.w));
+                p.out + ((int64_t)(d.row0 + token) * p.Hq + d.g * p.G + (r - token * p.G)) * kPagedDim +
+                4 * c) = make_uint2(Half16<BF>::pack(a.x, a.y), Half16<BF>::pack(a.z, a.w));
         }
         if (!meet(s, met)) return false;  // (the rows have been read)
     }
