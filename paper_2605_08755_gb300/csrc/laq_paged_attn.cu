@@ -16,8 +16,8 @@
 // tile are filled by boxes of a page each.  Rows of V past the request's last token are zeroed in
 // shared memory, since 0 * NaN would not vanish in the product.
 //
-// Work split: one CTA per SM walks an equal share of all items' tiles in order (a "unit" is a tile
-// of 128 tokens of an item; kStart more units stand for each item's start and end); an item that a share's border
+// Work split: one CTA per SM walks an equal share of all items' tiles in order (in units of what
+// tiles of 128 tokens, and starting and ending an item, cost); an item that a share's border
 // cuts is finished by its CTAs together: each writes its part's O, maximum and sum to the workspace,
 // and when all of them are there each adds up a share of the rows, in the order of the parts.
 #include <cuda.h>
@@ -46,8 +46,10 @@ constexpr int kQueue = 4;
 constexpr int kStaging = (2 + kStages) * kTileBytes;  // where: 4 KB for each softmax warp
 constexpr int kSmemTiles = kStaging + 8 * 4096;
 constexpr int kMostCtas = 192;          // so that a row of every part fits beside the others
-constexpr int kMinUnits = 2;            // for a CTA of its own (or one an item, if that is more CTAs)
-constexpr int kStart = 2;               // what starting and ending an item costs, in tiles
+// Units of work: of a tile of an item of two q tiles, of one of a single q tile, and of starting and
+// ending an item; and the fewest that a CTA of its own is for (fewer only down to an item a CTA).
+constexpr int kWide = 2, kNarrow = 1, kStart = 4, kMinUnits = 4;
+static_assert(kMinUnits >= kWide && kStart >= kWide, "a share inside an item has a tile of it");
 
 // The part of an item that one CTA works on: tiles lo .. hi - 1 of its nt (0: no row of it sees a token;
 // -1: the end of the CTA's share).
@@ -223,11 +225,14 @@ struct Req {
         const int end = past + min(n, (t + 1) * 2 * p.tau);
         return (max(end, 0) + kTile - 1) / kTile;
     }
+    __device__ int cost(const ChunkParams& p, int t) const {  // of a tile of item t
+        return n - t * 2 * p.tau <= p.tau ? kNarrow : kWide;
+    }
     // units of all items of one kv head
     __device__ long long units(const ChunkParams& p) const {
         long long sum = (long long)kStart * m;
 #pragma unroll 1
-        for (int t = 0; t < m; ++t) sum += tiles(p, t);
+        for (int t = 0; t < m; ++t) sum += cost(p, t) * tiles(p, t);
         return sum;
     }
 };
@@ -288,7 +293,8 @@ __device__ void walk_role(const ChunkParams& p, Bars* s) {
         // the warp adds up the items' units, 32 items at a time; a second time to find `into`
 #pragma unroll 1
         for (int pass = 0, t0 = 0;;) {
-            int v = t0 + lane < r.m ? kStart + r.tiles(p, t0 + lane) : 0, inc = v;
+            int v = t0 + lane < r.m ? kStart + r.cost(p, t0 + lane) * r.tiles(p, t0 + lane) : 0,
+                inc = v;
 #pragma unroll 1
             for (int o = 1; o < 32; o *= 2) {
                 const int y = __shfl_up_sync(0xffffffffu, inc, o);
@@ -327,9 +333,11 @@ __device__ void walk_role(const ChunkParams& p, Bars* s) {
             return;
         bool found = false;
         while (left > 0 && !found) {
-            const int nt = r.tiles(p, t), units = nt + kStart;
+            // (a tile is the CTA's whose share has its first unit)
+            const int nt = r.tiles(p, t), c = r.cost(p, t), units = kStart + c * nt;
             const int take = (int)min(left, (long long)(units - off));
-            const int lo = max(off - kStart, 0), hi = off + take - kStart;
+            const int lo = (max(off - kStart, 0) + c - 1) / c,
+                      hi = (max(off + take - kStart, 0) + c - 1) / c;
             found = hi > lo || (nt == 0 && off == 0);
             if (found) {
                 x->nt = nt;
@@ -349,7 +357,7 @@ __device__ void walk_role(const ChunkParams& p, Bars* s) {
                 x->index = 0;
                 if (x->split) {
                     x->first = shares.cta_of(U + kStart);
-                    x->parts = shares.cta_of(U + kStart + nt - 1) - x->first + 1;
+                    x->parts = shares.cta_of(U + kStart + c * (nt - 1)) - x->first + 1;
                     x->index = (int)blockIdx.x - x->first;
                     s->pend[x->slot] = *x;
                 }
