@@ -1,7 +1,7 @@
 // laq_paged_decode.cu -- attention of a few new tokens per request over the paged cache: up to 16 rows
 // (new tokens x q heads of a kv head), where reading K and V is what counts.
 //
-// A pair is (request, kv head).  CTAs of 8 warps, two per SM, walk equal shares of all pairs' tokens in
+// A pair is (request, kv head).  CTAs of 8 warps, one or two per SM, walk equal shares of all pairs' tokens in
 // order, in units of 128 tokens; within a CTA's part of a pair the warps take steps of 16 tokens in
 // turn.  A warp streams its steps' K and V (4 KB each, one TMA box per page and 64 dimensions) through a
 // ring of kSlots slots of its own and keeps the running maximum, sum and output of its tokens
@@ -523,7 +523,12 @@ laq_status launch_decode(const PagedKv& kv, bool bf, const void* q, int64_t q_st
     if (!encode_cache(&p.kmap, kv, bf, kv.k, box) || !encode_cache(&p.vmap, kv, bf, kv.v, box))
         return LAQ_ERR_CUDA;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(2 * sms));
+    // Two CTAs an SM fill the gaps at the ends of parts; where few pairs leave a CTA one part or two, one CTA
+    // an SM makes fewer parts to add, and leaves room for the next kernel's to start: us at two / one, 8 kv
+    // heads, 1 x 2048 tokens 10.1 / 9.5, 1 x 65,537 58.5 / 49.1, 8 x 20,000 72 / 68, but 4 x 1000 11.1 /
+    // 12.5, 32 x 8192 98 / 101, 100 x 1500 69 / 75.
+    const int64_t pairs = (int64_t)kv.batch * kv.Hkv;
+    cfg.gridDim = dim3((unsigned)(8 * pairs <= sms ? sms : 2 * sms));
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = kSmem;
     cfg.stream = stream;
