@@ -500,10 +500,15 @@ def laq_argmax(logits, out=None, stream=None):
 
 # ---- a serving step over a paged cache ----
 
-def _dtype(t):
+@functools.lru_cache(maxsize=None)
+def _dtypes():
     import torch
+    return {torch.float16: F16, torch.bfloat16: BF16, torch.float32: F32}
+
+
+def _dtype(t):
     try:
-        return {torch.float16: F16, torch.bfloat16: BF16, torch.float32: F32}[t.dtype]
+        return _dtypes()[t.dtype]
     except KeyError:
         raise TypeError(f"fp16, bf16 or fp32 expected, not {t.dtype}") from None
 
@@ -513,7 +518,7 @@ def _typed(name, t, dtype, dense=True):
     ValueError: what the C ABI takes as a bare address is checked here."""
     if t is None:
         return
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise TypeError(f"{name}: {dtype} expected, not {t.dtype}")
     if dense and not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
@@ -562,19 +567,23 @@ def laq_paged_append(qkv, cache, Hq, theta, eps, q_norm_w=None, k_norm_w=None, q
     """qkv [T, (Hq + 2 Hkv) * 128] (rows may be strided) -> q_out [T, Hq, 128]: q and k normalised
     per head (where weights are given) and rotated, k and v stored in the cache's pages."""
     T, width = qkv.shape
+    dtype = cache.dtype
     if width != (Hq + 2 * cache.Hkv) * 128 or qkv.stride(1) != 1:
         raise ValueError("qkv [T, (Hq + 2 Hkv) * 128] expected")
-    for name, t in (("qkv", qkv), ("q_norm_w", q_norm_w), ("k_norm_w", k_norm_w)):
-        _typed(name, t, cache.dtype, dense=t is not qkv)
+    _typed("qkv", qkv, dtype, dense=False)
+    _typed("q_norm_w", q_norm_w, dtype)
+    _typed("k_norm_w", k_norm_w, dtype)
     if q_out is None:
         q_out = qkv.new_empty((T, Hq, 128))
     else:
-        _typed("q_out", q_out, cache.dtype)
+        _typed("q_out", q_out, dtype)
         if q_out.numel() != T * Hq * 128:
             raise ValueError("q_out [T, Hq, 128] expected")
-    _check(lib().laq_paged_append(cache.ref, _ptr(qkv), _row_stride(qkv, width), T, Hq,
-                                  _ptr(q_norm_w), _ptr(k_norm_w), theta, eps, _ptr(q_out),
-                                  _stream(stream)), "laq_paged_append")
+    st = lib().laq_paged_append(cache.ref, qkv.data_ptr(), _row_stride(qkv, width), T, Hq,
+                                _ptr(q_norm_w), _ptr(k_norm_w), theta, eps, q_out.data_ptr(),
+                                _stream(stream))
+    if st:
+        _check(st, "laq_paged_append")
     return q_out
 
 
@@ -600,10 +609,11 @@ def laq_paged_attention(q, cache, max_q, scale, workspace, out=None, stream=None
         _typed("out", out, cache.dtype)
         if out.numel() != T * Hq * 128:
             raise ValueError("out [T, Hq, 128] expected")
-    _check(lib().laq_paged_attention(cache.ref, _ptr(q), _row_stride(q, Hq * 128), T, max_q, Hq,
-                                     scale, _ptr(out), _ptr(workspace),
-                                     workspace.numel() * workspace.element_size(),
-                                     _stream(stream)), "laq_paged_attention")
+    st = lib().laq_paged_attention(cache.ref, q.data_ptr(), _row_stride(q, Hq * 128), T, max_q, Hq,
+                                   scale, out.data_ptr(), _ptr(workspace),
+                                   workspace.numel() * workspace.element_size(), _stream(stream))
+    if st:
+        _check(st, "laq_paged_attention")
     return out
 
 
@@ -619,16 +629,22 @@ def laq_sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, 
         raise ValueError("logits [M, V] with dense rows expected")
     if out is None:
         out = torch.empty((M,), dtype=torch.int32, device=logits.device)
-    f32, i32 = torch.float32, torch.int32
-    for name, t, dt in (("u", u, f32), ("temperature", temperature, f32), ("top_k", top_k, i32),
-                        ("top_p", top_p, f32), ("min_p", min_p, f32), ("out", out, i32),
-                        ("p_out", p_out, f32)):
-        _typed(name, t, dt)
-        if t is not None and t.shape != (M,):
-            raise ValueError(f"{name}: [{M}] expected")
-    _check(lib().laq_sample(_ptr(logits), _dtype(logits), M, V, _row_stride(logits, V),
-                            _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p), _ptr(u),
-                            _ptr(out), _ptr(p_out), _stream(stream)), "laq_sample")
+    ptrs = []
+    for t, dt in ((temperature, torch.float32), (top_k, torch.int32), (top_p, torch.float32),
+                  (min_p, torch.float32), (u, torch.float32), (out, torch.int32),
+                  (p_out, torch.float32)):
+        if t is None:
+            ptrs.append(None)
+            continue
+        if t.dtype is not dt or t.dim() != 1 or t.shape[0] != M or not t.is_contiguous():
+            raise (TypeError if t.dtype is not dt else ValueError)(
+                f"row settings, u, out and p_out: contiguous [{M}] expected (top_k and out int32, the "
+                f"others fp32), not {tuple(t.shape)} {t.dtype}")
+        ptrs.append(t.data_ptr())
+    st = lib().laq_sample(logits.data_ptr(), _dtype(logits), M, V, _row_stride(logits, V), *ptrs,
+                          _stream(stream))
+    if st:
+        _check(st, "laq_sample")
     return out
 
 
