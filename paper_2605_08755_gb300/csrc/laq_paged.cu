@@ -18,7 +18,7 @@ laq_status paged_kv(const laq_paged_kv* kv, int64_t T, int32_t Hq, PagedKv* out)
     if (kv->D != kPagedDim || kv->Hkv < 1 || kv->Hkv > 4096 || Hq < 1 || Hq % kv->Hkv ||
         Hq / kv->Hkv > 64 || P < 8 || P > 1024 || (P & (P - 1)) || T < 0 || T > most ||
         kv->batch < 0 || kv->batch > most || kv->pages < 1 || kv->pages > 0x7fffffff ||
-        kv->max_pages < 1 || kv->max_pages > 0x7fffffff / P || kv->table_stride < kv->max_pages ||
+        kv->max_pages < 1 || kv->max_pages > ((int64_t)1 << 30) / P || kv->table_stride < kv->max_pages ||
         kv->token_stride < kPagedDim || kv->head_stride < kPagedDim || kv->page_stride < kPagedDim ||
         kv->token_stride >= lim || kv->head_stride >= lim || kv->page_stride >= lim ||
         ((kv->token_stride | kv->head_stride | kv->page_stride) & 7) ||

@@ -903,7 +903,9 @@ __device__ void softmax_role(const ChunkParams& p, Bars* s, uint32_t smem, uint8
                     pk[e >> 1] = Half16<BF>::pack(v[e], v[e + 1]);
                 }
                 if (!trust) break;
-                if (!__any_sync(0xffffffffu, valid && (sum[0] + sum[1]) + (sum[2] + sum[3]) > most)) break;
+                // (a row without a maximum so far has none of its scores in units of one)
+                const float all = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                if (!__any_sync(0xffffffffu, valid && all > (m == -INFINITY ? 0.f : most))) break;
             }
             first = false;
             tm_st32(ts, pk);

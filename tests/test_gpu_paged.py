@@ -254,3 +254,43 @@ def test_append_page_outside_the_cache_and_rows_of_no_request():
     torch.cuda.synchronize()
     before[2, :, 3] = k[2, :, 3]
     assert torch.equal(k, before) and (q[3:] == 9).all() and not (q[:3] == 9).all()
+
+
+@pytest.mark.parametrize("n,L,Hkv", [([40], [1500], 1), ([200], [700], 2), ([2], [1500], 1)])
+def test_attention_where_early_keys_score_minus_infinity(n, L, Hkv):
+    """Keys of -inf in the first tiles (q positive): those tokens have weight 0 and leave a row without a
+    maximum until its first finite score."""
+    P, Hq = 16, 4 * Hkv
+    table, q_start, kv_len, pages = batch(n, L, P, 21)
+    k, v = make_cache(pages, Hkv, P, F16, 22)
+    q = torch.rand((sum(n), Hq, D), device="cuda").half() + 0.01
+    for t in range(400):
+        k[int(table[0, t // P]), :, t % P] = float("-inf")
+    cache = _lib.PagedCache(k, v, torch.from_numpy(table).cuda(), torch.from_numpy(q_start).cuda(),
+                            torch.from_numpy(kv_len).cuda())
+    ws = _lib.paged_attention_workspace(sum(n), 1, max(n), Hq, Hkv, "cuda")
+    out = _lib.laq_paged_attention(q, cache, max(n), SCALE, ws)
+    finite = k.clone()   # the same weights: far below every other key's
+    finite[finite == float("-inf")] = -1000.0
+    check_attention(out, q, finite, v, table, q_start, kv_len, SCALE, F16)
+
+
+@pytest.mark.parametrize("n,L", [([33], [33]), ([150, 1], [2500, 90])])
+def test_attention_of_scores_that_keep_growing(n, L):
+    """Keys that grow along the request, so that the maximum moves in most tiles, in small steps and in
+    large ones, up to scores of some hundreds."""
+    P, Hq, Hkv = 32, 4, 1
+    table, q_start, kv_len, pages = batch(n, L, P, 31)
+    k, v = make_cache(pages, Hkv, P, BF16, 32)
+    q = (2 * torch.randn((sum(n), Hq, D), device="cuda")).to(BF16)
+    for b, x in enumerate(L):
+        for t in range(x):
+            k[int(table[b, t // P]), :, t % P] *= 0.05 + 12.0 * t / x
+    cache = _lib.PagedCache(k, v, torch.from_numpy(table).cuda(), torch.from_numpy(q_start).cuda(),
+                            torch.from_numpy(kv_len).cuda())
+    ws = _lib.paged_attention_workspace(sum(n), len(n), max(n), Hq, Hkv, "cuda")
+    out = _lib.laq_paged_attention(q, cache, max(n), SCALE, ws)
+    # fp32 scores of a few hundred: 2^-24 of the products' sum, 128 of them, adds 2^-9 to a weight
+    ref, A = serving.paged_attention(f64(q), f64(k), f64(v), table, q_start, kv_len, SCALE)
+    u = UNIT[BF16]
+    assert np.all(np.abs(f64(out) - ref) <= u * np.abs(ref) + (u + 2.0 ** -8) * A + 2.0 ** -25)
