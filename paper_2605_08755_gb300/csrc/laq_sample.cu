@@ -4,10 +4,10 @@
 // Weights are whole numbers (2^40 for the maximum), so that every sum is exact, integer atomics give
 // one result in any order, and no result depends on how a row is split.  What top-k and top-p keep is
 // a prefix of the order (logit descending, index ascending), found in three steps:
-//   1. a histogram in 2048 bins of equal width below the row's maximum, whose prefix sums name the bin
-//      that the cut falls in.  For top-p: of every logit's weight and count.  For a small top-k: of the
-//      maxima that the threads have found, one each; where k of them lie above an edge, at least k
-//      logits do, and hardly more; else of every logit's count;
+//   1. a histogram in 2048 bins of equal width below the row's maximum (of every logit's weight and
+//      count for top-p, of its count for top-k), whose prefix sums name the bin that the cut falls in.  A
+//      small top-k needs none: the largest logits of groups of eight threads are known from the first
+//      pass, and at least k logits, and hardly more, are not below the k-th largest of these;
 //   2. the elements of that bin, or, where the whole prefix up to it is small (the usual case), all
 //      elements up to it, are gathered into a list;
 //   3. the list is ranked (by comparing all pairs, or sorted where it is long), and prefix sums in that
@@ -47,8 +47,10 @@ constexpr int kList = 2048;        // elements of the list
 constexpr int kIdxBits = 22;       // V <= 2^22
 constexpr int kMaxWarps = 32;
 constexpr int kMaxC = 8;
+constexpr int kGroup = 8;          // threads whose largest logit is kept
+static_assert(kGroup >= kMaxC, "");
+constexpr int kMaxGroups = 1024 / kGroup;
 constexpr int kPairs = 256;        // lists up to this are ranked by comparing all pairs
-constexpr int kSmallK = 512;       // top-k up to this starts from the threads' maxima
 
 struct SampleParams {
     const void* logits;
@@ -69,8 +71,9 @@ struct alignas(16) SampleSmem {
     };
     u64 list[kList];
     u64 red[kMaxWarps], red2[kMaxWarps];
-    float fred[kMaxWarps];
-    float ends[kMaxC];           // the largest element, then a bin, of every CTA of the cluster
+    float most[kMaxGroups];      // the groups' largest elements
+    float2 ends[kMaxC];          // every CTA's largest element, and a bound for a small top-k
+    u64 part_w[kMaxC], part_n[kMaxC];
     u64 sums[kMaxC];             // kept weight of every CTA
     u64 found[5], cut, part_of, need;
     uint32_t n_list, first, counts[kMaxC];
@@ -377,10 +380,11 @@ __global__ void __launch_bounds__(1024) sample_kernel(const SampleParams p) {
             row.n = chunks * kPer;  // (the last chunk's end is -inf in the copy)
         }
     }
-    const float thread_top = top;
+    const int k = k_in <= 0 || k_in > V ? V : k_in;
+    const int groups = nt / kGroup;
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-    if (lane == 0) s.fred[warp] = top;
+    for (int o = kGroup / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    if (tid % kGroup == 0) s.most[tid / kGroup] = top;
     if (tid == 0) {
         s.n_list = 0;
         s.first = 0xffffffffu;
@@ -393,15 +397,32 @@ __global__ void __launch_bounds__(1024) sample_kernel(const SampleParams p) {
     __syncthreads();
     // (every CTA of the cluster has to have started before its shared memory is written)
     if (C > 1) asm volatile("barrier.cluster.wait.aligned;\n" ::: "memory");
-    if (warp == 0) {
-        top = lane < nt / 32 ? s.fred[lane] : -INFINITY;
+    // The groups' largest elements, ranked: the first is the CTA's; not below the (k / C)-th lie at least k / C
+    // elements of this CTA, and hardly more where k / C is well below the number of groups.
+    const int nth = (k + C - 1) / C;
+    {
+        const int i = tid / kGroup;
+        const float x = s.most[i];
+        int above = 0;
+#pragma unroll 4
+        for (int j = tid % kGroup; j < groups; j += kGroup) {
+            const float y = s.most[j];
+            above += y > x || (y == x && j < i);
+        }
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-        if (lane < C) remote(&s.ends[0], lane)[rank] = top;
+        for (int o = kGroup / 2; o > 0; o >>= 1) above += __shfl_xor_sync(0xffffffffu, above, o);
+        const int r = tid % kGroup;  // (C <= kGroup: a lane a CTA)
+        if (above == 0 && r < C) remote(&s.ends[0], r)[rank].x = x;
+        if (above == min(nth, groups) - 1 && r < C)
+            remote(&s.ends[0], r)[rank].y = 2 * nth <= groups ? x : -INFINITY;
     }
     all_sync();
-    top = s.ends[0];
-    for (int r = 1; r < C; ++r) top = fmaxf(top, s.ends[r]);
+    top = s.ends[0].x;
+    float bound = s.ends[0].y;  // at least k elements are not below it (-inf: no such bound)
+    for (int r = 1; r < C; ++r) {
+        top = fmaxf(top, s.ends[r].x);
+        bound = fminf(bound, s.ends[r].y);
+    }
     if (top == -INFINITY) {  // (all CTAs of the cluster agree)
         if (rank == 0 && tid == 0) {
             p.out[m] = 0;
@@ -411,7 +432,6 @@ __global__ void __launch_bounds__(1024) sample_kernel(const SampleParams p) {
     }
 
     // ---- the row's settings ----
-    const int k = k_in <= 0 || k_in > V ? V : k_in;
     if (!(t_in > 0.f) || (k == 1 && V > 1) || V == 1) {  // the first maximum
         uint32_t first = 0xffffffffu;
         row.each([&](float x, int i) {
@@ -491,63 +511,79 @@ __global__ void __launch_bounds__(1024) sample_kernel(const SampleParams p) {
             atomicAdd(&s.cnt[b], 1u);
         }
     };
-    // The cluster's bins, added up in CTA 0: prefix sums of counts or weights, and the bin where they
-    // reach `need` (0: top-p's part of the sum over all bins).  found, in all CTAs: bin, what is left of
-    // the need in it, the elements of the bin, the elements up to and with it, the sum.
+    // The cluster's bins, a share of them added up by each CTA: prefix sums of counts or weights, and the
+    // bin where they reach `need` (0: top-p's part of the sum over all bins).  found, in all CTAs: bin,
+    // what is left of the need in it, the elements of the bin, the elements up to and with it, the sum.
     auto find_bin = [&](bool by_mass, u64 need) {
         all_sync();
-        if (C > 1) {
-            if (rank != 0)
+        // (of a CTA's bins only it reads the ones of its own share: they take the sums)
+        const int share = kBins / C, per = share > nt ? share / nt : 1;
+        const int b0 = rank * share + min(tid * per, share), b1 = rank * share + min((tid + 1) * per, share);
+        u64 sv = 0, sn = 0, sum, all;
 #pragma unroll 1
-                for (int b = tid; b < kBins; b += nt)
-                    if (s.cnt[b]) {
-                        atomicAdd(remote(&s.cnt[b], 0), s.cnt[b]);
-                        if (by_mass) {
-                            const uint32_t w = s.lo[b], old = atomicAdd(remote(&s.lo[b], 0), w);
-                            const uint32_t up = s.hi[b] + (old + w < old);
-                            if (up) atomicAdd(remote(&s.hi[b], 0), up);
-                        }
-                    }
-            cluster.sync();
+        for (int b = b0; b < b1; ++b) {
+            uint32_t n = s.cnt[b];
+            u64 v = by_mass ? (u64)s.lo[b] + ((u64)s.hi[b] << 32) : n;
+            if (C > 1) {
+                for (int i = 1; i < C; ++i) {
+                    const int r = (rank + i) & (C - 1);
+                    const uint32_t c = remote(s.cnt, r)[b];
+                    n += c;
+                    v += by_mass ? (u64)remote(s.lo, r)[b] + ((u64)remote(s.hi, r)[b] << 32) : c;
+                }
+                s.cnt[b] = n;
+                s.lo[b] = (uint32_t)v;
+                s.hi[b] = (uint32_t)(v >> 32);
+            }
+            sv += v;
+            sn += n;
         }
-        if (rank == 0) {
-            const int per = kBins / nt;  // nt divides kBins
-            u64 sv = 0, sn = 0, sum, all;
-#pragma unroll 1
-            for (int b = tid * per; b < (tid + 1) * per; ++b) {
-                sv += by_mass ? (u64)s.lo[b] + ((u64)s.hi[b] << 32) : s.cnt[b];
-                sn += s.cnt[b];
+        u64 at = block_scan(sv, s.red, &sum), en = block_scan(sn, s.red2, &all);
+        if (C > 1) {
+            if (tid < C) {
+                remote(s.part_w, tid)[rank] = sum;
+                remote(s.part_n, tid)[rank] = all;
             }
-            u64 at = block_scan(sv, s.red, &sum), en = block_scan(sn, s.red2, &all);
-            if (need == 0) need = max((u64)1, part(sum, pf));
-#pragma unroll 1
-            for (int b = tid * per; b < (tid + 1) * per; ++b) {
-                const u64 v = by_mass ? (u64)s.lo[b] + ((u64)s.hi[b] << 32) : s.cnt[b];
-                en += s.cnt[b];
-                if (at < need && need <= at + v)
-#pragma unroll 1
-                    for (int r = 0; r < C; ++r) {
-                        u64* f = remote(s.found, r);
-                        f[0] = b;
-                        f[1] = need - at;
-                        f[2] = s.cnt[b];
-                        f[3] = en;
-                        f[4] = sum;
-                    }
-                at += v;
+            cluster.sync();
+            sum = 0;
+            for (int r = 0; r < C; ++r) {
+                if (r < rank) {
+                    at += s.part_w[r];
+                    en += s.part_n[r];
+                }
+                sum += s.part_w[r];
             }
+        }
+        if (need == 0) need = max((u64)1, part(sum, pf));
+#pragma unroll 1
+        for (int b = b0; b < b1; ++b) {
+            const u64 v = by_mass || C > 1 ? (u64)s.lo[b] + ((u64)s.hi[b] << 32) : s.cnt[b];
+            en += s.cnt[b];
+            if (at < need && need <= at + v)
+#pragma unroll 1
+                for (int r = 0; r < C; ++r) {
+                    u64* f = remote(s.found, r);
+                    f[0] = b;
+                    f[1] = need - at;
+                    f[2] = s.cnt[b];
+                    f[3] = en;
+                    f[4] = sum;
+                }
+            at += v;
         }
         all_sync();
     };
     // Elements of bins first .. last (and of `prefix`, within what is kept) go to CTA 0's list (n_all, or as
     // many as it holds), the other CTAs' by way of their own (an atomic a element across the cluster stalls
-    // its warp for 1500 cycles).
+    // its warp for 1500 cycles).  With first < 0: all elements that are not below `bound`.
     uint32_t n_all = 0;
     auto gather = [&](int first, int last) {
         // (bounds outside the bins' edges spare most elements the exact test)
         const float slack = fabsf(top) * 0x1p-20f;
         auto edge = [&](int b, float e) { return top - b / scale * (1.f - e) + e * slack; };
-        const float lo = last >= kBins - 1 || !(scale > 0.f) ? -INFINITY : edge(last + 1, -0x1p-18f) - slack;
+        const float lo = first < 0 ? bound
+                         : last >= kBins - 1 || !(scale > 0.f) ? -INFINITY
+                                                               : edge(last + 1, -0x1p-18f) - slack;
         const float hi = first <= 1 || !(scale > 0.f) ? INFINITY : edge(first, 0x1p-18f) + slack;
         constexpr int kPer = Row<DT>::kPer;
         const int chunks = (row.n + kPer - 1) / kPer;
@@ -561,7 +597,7 @@ __global__ void __launch_bounds__(1024) sample_kernel(const SampleParams p) {
 #pragma unroll
             for (int k = 0; k < kPer; ++k)
                 if (x[k] >= lo && x[k] <= hi) {
-                    const int b = bin_of(x[k]);
+                    const int b = first < 0 ? first : bin_of(x[k]);
                     const u64 at_place = place(x[k], row.i0 + kPer * c + k);
                     if (b >= first && b <= last && at_place >= cut &&
                         (shift == kPlaceBits || (at_place >> shift) == prefix)) {
@@ -597,34 +633,12 @@ __global__ void __launch_bounds__(1024) sample_kernel(const SampleParams p) {
     // ---- the cuts ----  phase 0: a small top-k, 1: top-k, 2: top-p
     u64 total = 0;          // the sum that top-p's part is of, where it is not top-k's list's
     bool in_list = false;   // CTA 0's list has all that can be kept (n_all elements, some not kept)
-    for (int phase = k < V ? k <= kSmallK ? 0 : 1 : use_p ? 2 : 3; phase < 3;) {
+    for (int phase = k < V ? bound > -INFINITY ? 0 : 1 : use_p ? 2 : 3; phase < 3;) {
         bool whole = true;
         level = 0;
         shift = kPlaceBits;
         if (phase == 0) {
-            // k elements at least, and hardly more: each CTA's bin up to which the maxima of k / C of its
-            // threads lie, and of these bins the last
-            scale = kBins / 64.f;
-            if (thread_top > -INFINITY) atomicAdd(&s.cnt[bin_of(thread_top)], 1u);
-            if (tid == 0) s.found[0] = kBins;
-            __syncthreads();
-            const u64 need = (u64)((k + C - 1) / C);
-            const int per = kBins / nt;
-            u64 sum = 0, all;
-#pragma unroll 1
-            for (int b = tid * per; b < (tid + 1) * per; ++b) sum += s.cnt[b];
-            u64 at = block_scan(sum, s.red, &all);
-#pragma unroll 1
-            for (int b = tid * per; b < (tid + 1) * per; ++b) {
-                if (at < need && need <= at + s.cnt[b]) s.found[0] = b;
-                at += s.cnt[b];
-            }
-            __syncthreads();
-            if (tid < C) remote(s.ends, tid)[rank] = (float)s.found[0];
-            all_sync();
-            float most = s.ends[0];
-            for (int r = 1; r < C; ++r) most = fmaxf(most, s.ends[r]);
-            bin = (int)most;
+            bin = -1;
         } else {
             // (weights vanish 27.8 t below the maximum)
             const bool by_mass = phase == 2;
@@ -653,9 +667,9 @@ __global__ void __launch_bounds__(1024) sample_kernel(const SampleParams p) {
             }
             if (rank == 0 && tid == 0) s.need = need;
         }
-        if (phase > 0 || bin < kBins - 1) gather(whole ? 0 : bin, bin);
+        gather(phase == 0 ? -1 : whole ? 0 : bin, bin);
         if (phase == 0) {
-            in_list = bin < kBins - 1 && n_all <= kList;
+            in_list = n_all <= kList;
             if (in_list) break;
             phase = 1;
         } else if (whole) {
@@ -696,23 +710,23 @@ __global__ void __launch_bounds__(1024) sample_kernel(const SampleParams p) {
         const bool by_k = k < V;
         const bool second = cut != 0;  // the list is top-p's, of what top-k kept
         if (n <= kPairs) {
-            // four lanes an element: its rank and what comes before it in the order
-            const int q = tid & 3;
+            // eight lanes an element: its rank and what comes before it in the order
+            const int q = tid & 7;
             for (int i = tid; i < n; i += nt) s.w[i] = weight(place_logit(s.list[i]));
             __syncthreads();
-            for (int i0 = 0; i0 < n; i0 += nt / 4) {
-                const int i = i0 + (tid >> 2);
+            for (int i0 = 0; i0 < n; i0 += nt / 8) {
+                const int i = i0 + (tid >> 3);
                 const u64 mine = i < n ? s.list[i] : 0;
                 u64 before = 0;
                 int rank_i = 0;
 #pragma unroll 4
-                for (int j = q; j < n; j += 4) {
+                for (int j = q; j < n; j += 8) {
                     const u64 c = s.list[j], w = s.w[j];
                     before += c > mine ? w : 0;
                     rank_i += c > mine;
                 }
 #pragma unroll
-                for (int o = 1; o < 4; o *= 2) {
+                for (int o = 1; o < 8; o *= 2) {
                     before += __shfl_xor_sync(0xffffffffu, before, o);
                     rank_i += __shfl_xor_sync(0xffffffffu, rank_i, o);
                 }
@@ -732,18 +746,18 @@ __global__ void __launch_bounds__(1024) sample_kernel(const SampleParams p) {
                     (!by_k || rank_i < (u64)k) && before < target && w >= floor_w ? w : 0;
             }
             __syncthreads();
-            for (int i0 = 0; i0 < n; i0 += nt / 4) {  // what is kept at smaller indices, and in all
-                const int i = i0 + (tid >> 2);
+            for (int i0 = 0; i0 < n; i0 += nt / 8) {  // what is kept at smaller indices, and in all
+                const int i = i0 + (tid >> 3);
                 const int idx = i < n ? place_index(s.list[i]) : 0;
                 u64 before = 0, all = 0;
 #pragma unroll 4
-                for (int j = q; j < n; j += 4) {
+                for (int j = q; j < n; j += 8) {
                     const u64 w = s.list[3 * kPairs + j];
                     all += w;
                     before += place_index(s.list[j]) < idx ? w : 0;
                 }
 #pragma unroll
-                for (int o = 1; o < 4; o *= 2) {
+                for (int o = 1; o < 8; o *= 2) {
                     before += __shfl_xor_sync(0xffffffffu, before, o);
                     all += __shfl_xor_sync(0xffffffffu, all, o);
                 }
