@@ -23,6 +23,10 @@
 // one number, so it is formed from the rounded reciprocal with one correction (Markstein, IBM J. Res.
 // Dev. 34, 1990), which gives the correctly rounded quotient.  A weight's whole number is its float's
 // significand, shifted: the conversion instruction to 64 bits runs on the few fp64 units.
+//   Bound: neither HBM nor one pipe, but a row's phases one after another, each ended by a meeting of a
+// CTA or a cluster, and in the passes over the logits the issue of instructions (a weight about 40
+// cycles for 32 logits, a place in the histogram 20).  Measured: 64 rows of 151,936 fp16 logits, each
+// with settings of its own, 51 us; one row 10 us; 257 rows of 32,003 fp32 logits 47 us.
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -903,13 +907,21 @@ laq_status launch_sample(SampleParams p, int64_t M, void* stream) {
     const int size = Logits<DT>::kSize;
     int C = 1;
     auto slice_of = [&](int c) { return (int)((((int64_t)p.V + c - 1) / c + 7) / 8 * 8); };
+    // CTAs of a row: until the next power of two passes two CTAs an SM in all (rows cost up to four times as
+    // much as others, by their settings: narrower CTAs in more than one wave even that out) or slices of
+    // 4096 logits.  Measured, us with the last step / without it: 64 x 151,936 51 / 64, 40 x 151,936 40 /
+    // 49, 16 x 32,000 in fp32 15 / 18, 1 x 32,000 8.6 / 11; with one step more 64 x 32,000 28 / 18, 257 x 32,003
+    // 51 / 47.
     while (C < kMaxC && ((int64_t)slice_of(C) * size > kSliceBytes ||
-                         (M * C * 2 <= sms && slice_of(C) > 4096)))
+                         (M * C <= sms && slice_of(C) > 4096)))
         C *= 2;
     p.C = C;
     p.slice = slice_of(C);
     p.resident = (int64_t)p.slice * size <= kSliceBytes;
-    const int threads = p.slice > 8192 ? 1024 : p.slice > 2048 ? 512 : 256;
+    // (1024 threads end a long slice's passes sooner, 512 meet sooner, and in half the registers: us at 1024 /
+    // 512, slices of 1000 8.6 / 6.7, 8000 23 / 17, 19,000 12.5 / 11.4, 32,003 47 / 61; at 256 8.0, 21, 14,
+    // 102)
+    const int threads = p.slice > 20480 ? 1024 : 512;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(M * C));
     cfg.blockDim = dim3((unsigned)threads);
