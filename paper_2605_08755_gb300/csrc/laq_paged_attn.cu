@@ -20,6 +20,20 @@
 // tiles of 128 tokens, and starting and ending an item, cost); an item that a share's border
 // cuts is finished by its CTAs together: each writes its part's O, maximum and sum to the workspace,
 // and when all of them are there each adds up a share of the rows, in the order of the parts.
+//
+// Bound: a tile's chain.  S (512 cycles of the tensor core), its exponentials (about 1250), P V (512)
+// and the hand-overs between them (about 500) follow one another; two q tiles in turn make that one
+// pair of tiles in about 2900 cycles, of which 2048 are products.  The two S and the two O fill tensor
+// memory, P being in S's place, so a third tile has no room; exponentials that cost almost nothing
+// gained 10 %.  Measured, 32 q heads on 8 kv heads: 8192 new tokens of 8192 in 400 us (1.37 PFLOP/s,
+// 72 % of the measured matrix rate; 428 us where the card has been at work for seconds and its clock
+// falls), 1024 of 16,384 in 196 us (1.36 PFLOP/s), 509 of 4093 beside 31 single tokens of up to 4096
+// in 87 us.  Small calls are bound by code that runs once: the walk to the first item, the first loads,
+// the parts' meeting.
+//   Tried and slower (8192 tokens): four warpgroups of softmax, half a row each (spills: 677 us), and P
+// handed over in halves (421 us).
+//   Precision: the tensor core cuts off what does not fit when it adds to O, about 2.7e-9 of O for each
+// cached token of a part: -9e-5 relative at 32,768 tokens in one part, a fifth of fp16's finest spacing.
 #include <cuda.h>
 #include <math.h>
 
@@ -719,103 +733,103 @@ __device__ __noinline__ bool end_piece(Bars* s, uint8_t* staging, uint32_t tmem,
     const int r_item = narrow ? r : wg * per + r;
     const bool valid = r < per && r_item < x.ntok * p.G;
     const bool busy = __any_sync(0xffffffffu, valid);
-            uint8_t* orow = valid ? reinterpret_cast<uint8_t*>(
-                                        p.out + ((int64_t)(x.row0 + r_item / p.G) * p.Hq + x.g * p.G +
-                                                 r_item % p.G) * kPagedDim)
-                                  : nullptr;
-            const uint32_t mine = s32(staging) + (threadIdx.x >> 5) * 4096;
-            tc_after();
-            float inv = l == 0.f ? 0.f : 1.f / l;
-            if (x.nt == 0 || (!narrow && !x.split)) {  // (no token: nothing was summed)
-                for (int q = 0; busy && q < 2; ++q) {
-                    uint4 c[8] = {};
-                    if (!first) {
-    #pragma unroll
-                        for (int k = 0; k < 2; ++k) {
-                            float o[32];
-                            tm_ld32(to + 64 * q + 32 * k, o);
-                            tm_wait_ld();
-                            pin32(o);
-    #pragma unroll
-                            for (int e = 0; e < 4; ++e)
-                                c[4 * k + e] = pack8<BF>(o + 8 * e, inv);
-                        }
-                    }
-                    put_rows(mine, c, narrow && wg ? nullptr : orow ? orow + 128 * q : nullptr);
-                }
-            } else if (x.split) {  // the others' parts are looked for at the end of the share
-                const int64_t part =
-                    (2 * (int64_t)blockIdx.x + x.slot) * 2 * p.part_rows + wg * p.part_rows + r;
-                for (int q = 0; busy && !first && q < 4; ++q) {
+    uint8_t* orow = valid ? reinterpret_cast<uint8_t*>(
+                                p.out + ((int64_t)(x.row0 + r_item / p.G) * p.Hq + x.g * p.G +
+                                         r_item % p.G) * kPagedDim)
+                          : nullptr;
+    const uint32_t mine = s32(staging) + (threadIdx.x >> 5) * 4096;
+    tc_after();
+    float inv = l == 0.f ? 0.f : 1.f / l;
+    if (x.nt == 0 || (!narrow && !x.split)) {  // (no token: nothing was summed)
+        for (int q = 0; busy && q < 2; ++q) {
+            uint4 c[8] = {};
+            if (!first) {
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
                     float o[32];
-                    tm_ld32(to + 32 * q, o);
+                    tm_ld32(to + 64 * q + 32 * k, o);
                     tm_wait_ld();
                     pin32(o);
-                    uint4 c[8];
-    #pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        c[e] = make_uint4(__float_as_uint(o[4 * e]), __float_as_uint(o[4 * e + 1]),
-                                          __float_as_uint(o[4 * e + 2]), __float_as_uint(o[4 * e + 3]));
-                    put_rows(mine, c,
-                             valid ? reinterpret_cast<uint8_t*>(p.part + part * kPagedDim + 32 * q)
-                                   : nullptr);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        c[4 * k + e] = pack8<BF>(o + 8 * e, inv);
                 }
-                if (valid) __stcg(&p.ml[part], make_float2(m, l));
-                __threadfence();
-                if (!meet(s, met)) return false;
-                if (threadIdx.x == 0) atomicAdd(&s->c.count[x.first], 1u);
-            } else {  // a narrow item of this CTA alone: the second warpgroup's sums by way of staging
-                float f0 = 0.f, f1 = 0.f;
-                for (int q = 0; q < 4; ++q) {
-                    float o[32];
-                    if (busy && !first) {
-                        tm_ld32(to + 32 * q, o);
-                        tm_wait_ld();
-                        pin32(o);
-                    }
-                    float4* slot = reinterpret_cast<float4*>(staging + (q & 1) * 16384 + r * 128);
-                    if (wg == 1) {
-                        if (q == 0) s->ml[r] = make_float2(m, l);
-                        if (busy && !first)
-    #pragma unroll
-                            for (int e = 0; e < 8; ++e)
-                                slot[e ^ (r & 7)] = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2],
-                                                                o[4 * e + 3]);
-                    }
-                    if (!meet(s, met)) return false;  // (two buffers: one meeting a round is enough)
-                    if (wg == 0 && busy) {
-                        if (q == 0) {
-                            const float2 b = s->ml[r];
-                            const float M = fmaxf(m, b.x);
-                            f0 = l == 0.f ? 0.f : ex2((m - M) * c);
-                            f1 = b.y == 0.f ? 0.f : ex2((b.x - M) * c);
-                            const float sum = fmaf(l, f0, b.y * f1);
-                            inv = sum == 0.f ? 0.f : 1.f / sum;
-                            f0 *= inv;
-                            f1 *= inv;
-                        }
-                        uint4 u[4];
-    #pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            float4 b = make_float4(0.f, 0.f, 0.f, 0.f);
-                            if (f1 != 0.f) b = slot[e ^ (r & 7)];
-                            o[4 * e] = fmaf(b.x, f1, o[4 * e] * f0);
-                            o[4 * e + 1] = fmaf(b.y, f1, o[4 * e + 1] * f0);
-                            o[4 * e + 2] = fmaf(b.z, f1, o[4 * e + 2] * f0);
-                            o[4 * e + 3] = fmaf(b.w, f1, o[4 * e + 3] * f0);
-                        }
-    #pragma unroll
-                        for (int e = 0; e < 4; ++e) u[e] = pack8<BF>(o + 8 * e, 1.f);
-                        if (valid)
-    #pragma unroll
-                            for (int e = 0; e < 4; ++e)
-                                *reinterpret_cast<uint4*>(orow + 64 * q + 16 * e) = u[e];
-                    }
-                    __syncwarp();
-                }
-                if (!meet(s, met)) return false;  // (staging is free again)
             }
-            tc_before();  // (the next item's first product comes after the next P)
+            put_rows(mine, c, narrow && wg ? nullptr : orow ? orow + 128 * q : nullptr);
+        }
+    } else if (x.split) {  // the others' parts are looked for at the end of the share
+        const int64_t part =
+            (2 * (int64_t)blockIdx.x + x.slot) * 2 * p.part_rows + wg * p.part_rows + r;
+        for (int q = 0; busy && !first && q < 4; ++q) {
+            float o[32];
+            tm_ld32(to + 32 * q, o);
+            tm_wait_ld();
+            pin32(o);
+            uint4 c[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                c[e] = make_uint4(__float_as_uint(o[4 * e]), __float_as_uint(o[4 * e + 1]),
+                                  __float_as_uint(o[4 * e + 2]), __float_as_uint(o[4 * e + 3]));
+            put_rows(mine, c,
+                     valid ? reinterpret_cast<uint8_t*>(p.part + part * kPagedDim + 32 * q)
+                           : nullptr);
+        }
+        if (valid) __stcg(&p.ml[part], make_float2(m, l));
+        __threadfence();
+        if (!meet(s, met)) return false;
+        if (threadIdx.x == 0) atomicAdd(&s->c.count[x.first], 1u);
+    } else {  // a narrow item of this CTA alone: the second warpgroup's sums by way of staging
+        float f0 = 0.f, f1 = 0.f;
+        for (int q = 0; q < 4; ++q) {
+            float o[32];
+            if (busy && !first) {
+                tm_ld32(to + 32 * q, o);
+                tm_wait_ld();
+                pin32(o);
+            }
+            float4* slot = reinterpret_cast<float4*>(staging + (q & 1) * 16384 + r * 128);
+            if (wg == 1) {
+                if (q == 0) s->ml[r] = make_float2(m, l);
+                if (busy && !first)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        slot[e ^ (r & 7)] = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2],
+                                                        o[4 * e + 3]);
+            }
+            if (!meet(s, met)) return false;  // (two buffers: one meeting a round is enough)
+            if (wg == 0 && busy) {
+                if (q == 0) {
+                    const float2 b = s->ml[r];
+                    const float M = fmaxf(m, b.x);
+                    f0 = l == 0.f ? 0.f : ex2((m - M) * c);
+                    f1 = b.y == 0.f ? 0.f : ex2((b.x - M) * c);
+                    const float sum = fmaf(l, f0, b.y * f1);
+                    inv = sum == 0.f ? 0.f : 1.f / sum;
+                    f0 *= inv;
+                    f1 *= inv;
+                }
+                uint4 u[4];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    float4 b = make_float4(0.f, 0.f, 0.f, 0.f);
+                    if (f1 != 0.f) b = slot[e ^ (r & 7)];
+                    o[4 * e] = fmaf(b.x, f1, o[4 * e] * f0);
+                    o[4 * e + 1] = fmaf(b.y, f1, o[4 * e + 1] * f0);
+                    o[4 * e + 2] = fmaf(b.z, f1, o[4 * e + 2] * f0);
+                    o[4 * e + 3] = fmaf(b.w, f1, o[4 * e + 3] * f0);
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) u[e] = pack8<BF>(o + 8 * e, 1.f);
+                if (valid)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        *reinterpret_cast<uint4*>(orow + 64 * q + 16 * e) = u[e];
+            }
+            __syncwarp();
+        }
+        if (!meet(s, met)) return false;  // (staging is free again)
+    }
+    tc_before();  // (the next item's first product comes after the next P)
     return true;
 }
 
@@ -1019,7 +1033,6 @@ __global__ void __launch_bounds__(kThreads, 1) paged_chunk_kernel(
                      : "memory");
     if (threadIdx.x == 0 && s->abort) atomicExch(p.status, (uint32_t)LAQ_ERR_TIMEOUT);
 }
-
 
 int part_rows(int64_t max_q, int G) {
     const int64_t per = 128 / G * G, rows = max_q * G;

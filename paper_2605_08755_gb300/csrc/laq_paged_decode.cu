@@ -14,6 +14,11 @@
 // The maximum moves only when a row's has grown by 2^8 (all of a warp's rows then rescale).
 //   The warps meet in shared memory, each in its own ring.  A pair that a share's border cuts is added
 // up by the last of its CTAs to finish, from the parts in the workspace in their order.
+//   Bound: HBM.  Measured, 32 q heads on 8 kv heads: 32 requests of 750 to 8192 tokens 97.7 us (587 MB,
+// 6.0 TB/s, 89 % of the measured copy rate), one of 65,537 48.1 us (5.6 TB/s), one of 2048 8.2 us, where
+// the launch, the first loads and the meeting of the parts are the time.  Steps of 16 tokens a warp, not
+// tiles of a CTA: no warp waits for another before the end of a pair.  The tokens are the product's 16
+// rows, so that 8 rows of q fill its columns (as its rows they would leave half of it empty).
 #include <cuda.h>
 #include <math.h>
 
