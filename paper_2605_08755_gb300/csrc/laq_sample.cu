@@ -17,8 +17,8 @@
 // otherwise a last pass sums the kept weights in the order of the index.
 //
 // A cluster of C CTAs works on a row, each on a slice that it reads once and keeps in shared memory
-// (a slice that does not fit is read again, from L2).  Histograms and the list meet in CTA 0, by
-// distributed shared memory.
+// (a slice that does not fit is read again, from L2).  By distributed shared memory each CTA adds up a share
+// of the histograms' bins, and the list meets in CTA 0.
 // The quotient (x - top) / t costs a compiler's division ten instructions for each logit; a row's t is
 // one number, so it is formed from the rounded reciprocal with one correction (Markstein, IBM J. Res.
 // Dev. 34, 1990), which gives the correctly rounded quotient.  A weight's whole number is its float's
